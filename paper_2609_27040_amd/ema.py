@@ -71,12 +71,22 @@ class SlabReclaimResult(ctypes.Structure):
                 ("released", ctypes.c_int32)]
 
 
+class KVTablesArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in (
+        "block_ids", "seq_lens", "new_lens", "staging_ids", "canon_table", "block_table",
+        "query_start", "slot_map", "prefetch_src", "prefetch_dst", "prefetch_n", "writeback_src",
+        "writeback_dst", "writeback_n")]
+        + [(n, ctypes.c_int32) for n in ("layers", "batch", "max_blocks", "n_ids", "n_slots",
+                                         "staging_slots", "stage_n", "writeback_cap")])
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with __graft_entry__.build() "
                           "(python -m paper_2609_27040_amd.build)")
     lib = ctypes.CDLL(LIB_PATH)
     P, I32, I64, SZ, U32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_uint32
+    F32C, PSZ = ctypes.c_float, ctypes.POINTER(ctypes.c_size_t)
     sig = {
         "ema_slice_create": [ctypes.POINTER(KVShape), SZ, SZ, U32, ctypes.POINTER(P)],
         "ema_slice_destroy": [P],
@@ -103,6 +113,18 @@ def _load():
         "ema_slab_group_runs": [P, I32, I32, P, P, P, I32, ctypes.POINTER(I32)],
         "ema_slab_prefetch_group": [P, I32, I32, I32, P],
         "ema_slab_reclaim": [P, I32, P, I64, P, ctypes.POINTER(SlabReclaimResult), P, I32, P, I32],
+        "ema_kv_tables_workspace": [P, P, PSZ],
+        "ema_kv_tables": [P, P, P, SZ, P],
+        "ema_kv_store": [P, P, I64, P, I64, P, I32, P],
+        "ema_paged_prompt_workspace": [P, I32, I32, I32, I32, PSZ],
+        "ema_paged_prompt_attention": [P, P, I64, P, P, P, I32, I32, I32, I32, F32C, P, I32, P,
+                                       SZ, P],
+        "ema_paged_diff_workspace": [P, I32, I32, I32, PSZ],
+        "ema_paged_diff_attention": [P, P, I64, P, P, I32, I32, I32, F32C, P, P, F32C, P, I32, P,
+                                     SZ, P],
+        "ema_paged_diff_prompt_workspace": [P, I32, I32, I32, I32, PSZ],
+        "ema_paged_diff_prompt_attention": [P, P, I64, P, P, P, I32, I32, I32, I32, F32C, P, P,
+                                            F32C, P, I32, P, SZ, P],
         "ema_sched_create": [I32, I32, I64, ctypes.POINTER(P)],
         "ema_sched_destroy": [P],
         "ema_sched_place": [P, I32, I32, I32, I64, P, ctypes.POINTER(I32)],
@@ -403,6 +425,218 @@ def slice_device_errors(h):
     c = ctypes.c_int32()
     _check(_lib.ema_slice_device_errors(h, ctypes.byref(c)))
     return c.value
+
+
+# ---- prompts and differential attention (include/ema_ops.h) --------------------------
+
+def _scratch(nbytes, workspace, stream, device):
+    """(tensor, address, bytes) of a call's workspace: the caller's, or one from
+    torch's allocator."""
+    if workspace is None:
+        if nbytes == 0:
+            return None, None, 0
+        import torch
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if stream != _torch().stream():
+            # allocated for the current stream, used on another
+            workspace.record_stream(torch.cuda.ExternalStream(stream))
+    n = workspace.numel() * workspace.element_size()
+    if n < nbytes:
+        _bad(f"workspace: {n} bytes, {nbytes} needed")
+    return workspace, _dev(workspace, "workspace", (workspace.dtype,)), n
+
+
+def _i32_out(t, name, host, shape):
+    """An int32 array of exactly this shape."""
+    if tuple(t.shape) != tuple(shape):
+        _bad(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if host:
+        if not isinstance(t, np.ndarray) or t.dtype != np.int32 or not t.flags.c_contiguous:
+            _bad(f"{name}: expected a contiguous int32 numpy array")
+        return t.ctypes.data
+    return _i32_dev(t, name)
+
+
+def _tables_args(h, block_ids, seq_lens, new_lens, block_table, slot_map, query_start, canon_table,
+                 staging, prefetch, writeback):
+    host = _host_only(h)
+    L, B, max_blocks = (int(x) for x in block_table.shape)
+    a = KVTablesArgs(layers=L, batch=B, max_blocks=max_blocks, n_ids=int(block_ids.shape[-1]),
+                     n_slots=int(slot_map.shape[-1]))
+    put = lambda field, t, shape: setattr(a, field, _i32_out(t, field, host, shape))
+    put("block_ids", block_ids, (L, a.n_ids))
+    put("seq_lens", seq_lens, (B,))
+    put("new_lens", new_lens, (B,))
+    put("block_table", block_table, (L, B, max_blocks))
+    put("query_start", query_start, (B + 1,))
+    put("slot_map", slot_map, (L, a.n_slots))
+    if canon_table is not None:
+        put("canon_table", canon_table, (L, B, max_blocks))
+    if staging is not None:
+        if prefetch is None or writeback is None:
+            _bad("staging needs the prefetch and writeback lists")
+        a.staging_slots, a.stage_n = (int(x) for x in staging.shape)
+        a.writeback_cap = int(writeback[0].shape[-1])
+        put("staging_ids", staging, (a.staging_slots, a.stage_n))
+        for kind, lists, n in (("prefetch", prefetch, a.stage_n),
+                               ("writeback", writeback, a.writeback_cap)):
+            for end, t, shape in zip(("src", "dst", "n"), lists, ((L, n), (L, n), (L,))):
+                put(f"{kind}_{end}", t, shape)
+    return a
+
+
+def kv_tables_workspace(h, args):
+    """Bytes of workspace for a KVTablesArgs."""
+    n = ctypes.c_size_t()
+    _check(_lib.ema_kv_tables_workspace(h, ctypes.byref(args), ctypes.byref(n)))
+    return n.value
+
+
+def kv_tables(h, block_ids, seq_lens, new_lens, block_table, slot_map, query_start,
+              canon_table=None, staging=None, prefetch=None, writeback=None, workspace=None,
+              stream=None):
+    """The tables of a step for all layers, from the requests' lengths: block_ids
+    [L][n_ids], seq_lens and new_lens [B] in; block_table [L][B][max_blocks],
+    slot_map [L][n_slots], query_start [B + 1] and, if given, canon_table out.
+    With ``staging`` [slots][stage_n] slice blocks are named by their staged copies,
+    and ``prefetch`` (src [L][stage_n], dst, count [L]) and ``writeback`` (src
+    [L][cap], dst, count [L]) are written. int32 device tensors (numpy arrays for
+    a host-only slice, which only validates)."""
+    a = _tables_args(h, block_ids, seq_lens, new_lens, block_table, slot_map, query_start,
+                     canon_table, staging, prefetch, writeback)
+    if _host_only(h):
+        _check(_lib.ema_kv_tables(h, ctypes.byref(a), None, 0, None))
+        return
+    st = _stream(stream)
+    ws, p, n = _scratch(kv_tables_workspace(h, a), workspace, st, block_table.device)
+    _check(_lib.ema_kv_tables(h, ctypes.byref(a), p, n, st))
+
+
+def _rows16(t, name, rec, heads):
+    """(address, elements between tokens) of a 16-bit GPU tensor [T][heads][128]
+    whose tokens may lie apart."""
+    T = _torch()
+    if not isinstance(t, T.Tensor) or not t.is_cuda:
+        _bad(f"{name}: expected a GPU tensor, got {type(t).__name__}")
+    if t.dtype not in _kv16_types(rec):
+        _bad(f"{name}: dtype {t.dtype} not in {_kv16_types(rec)}")
+    if t.dim() != 3 or t.shape[2] != 128 or (heads and t.shape[1] != heads):
+        _bad(f"{name}: shape {tuple(t.shape)}, expected [tokens][{heads or 'heads'}][128]")
+    stride = t.stride()
+    if t.numel() and (stride[2] != 1 or (t.shape[1] > 1 and stride[1] != 128)):
+        _bad(f"{name}: a token's heads are not contiguous")
+    return t.data_ptr(), (int(stride[0]) if t.shape[0] > 1 else int(t.shape[1]) * 128)
+
+
+def kv_store(h, k_new, v_new, slot_map, stream=None):
+    """k_new, v_new [T][Hkv][128] (16-bit; a token's heads contiguous, tokens any
+    multiple of 8 elements apart), slot_map int32 [T] (-1: not stored): device
+    tensors (a host-only slice takes slot_map as a numpy array and validates it)."""
+    if _host_only(h):
+        slots = _i32_host(slot_map)
+        row = int(_HANDLES[h][2]) * 128 if h in _HANDLES else 64 * 128
+        _check(_lib.ema_kv_store(h, None, row, None, row, slots.ctypes.data, len(slots), None))
+        return
+    rec = _HANDLES.get(h)
+    heads = rec[2] if rec else 0
+    k, ks = _rows16(k_new, "k_new", rec, heads)
+    v, vs = _rows16(v_new, "v_new", rec, heads)
+    T = int(k_new.shape[0])
+    if v_new.shape != k_new.shape:
+        _bad(f"v_new: shape {tuple(v_new.shape)}, k_new has {tuple(k_new.shape)}")
+    if slot_map.numel() != T:
+        _bad(f"slot_map: {slot_map.numel()} slots, {T} tokens")
+    _check(_lib.ema_kv_store(h, k, ks, v, vs, _i32_dev(slot_map, "slot_map", T), T,
+                             _stream(stream)))
+
+
+def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out, scale, lam,
+                  norm_weight, norm_eps, workspace, stream):
+    T = _torch()
+    rows, Hq = int(q.shape[0]), int(q.shape[1])
+    if len(block_table.shape) != 2:
+        _bad("block_table: expected [batch][max_blocks]")
+    B, max_blocks = int(block_table.shape[0]), int(block_table.shape[1])
+    extra = () if maps == 1 else (None, None, float(norm_eps))
+    sizes = (rows, B, Hq, max_blocks) if query_start is not None else (B, Hq, max_blocks)
+    if query_start is None and rows != B:
+        _bad(f"q: {rows} rows, {B} sequences")
+    if _host_only(h):
+        table, lens = _i32_host(block_table), _i32_host(seq_lens)
+        starts = () if query_start is None else (_i32_host(query_start).ctypes.data,)
+        _check(fn(h, None, Hq * 128, *starts, table.ctypes.data, lens.ctypes.data, *sizes,
+                  float(scale), *extra, None, F32, None, 0, None))
+        return
+    rec = _HANDLES.get(h)
+    code = T.out_codes.get(out.dtype)
+    if code is None:
+        _bad(f"out: dtype {out.dtype} not in {T.out_types}")
+    qp, qs = _rows16(q, "q", rec, 0)
+    starts = () if query_start is None else (_i32_dev(query_start, "query_start", B + 1),)
+    table = _i32_dev(block_table, "block_table", B * max_blocks)
+    lens = _i32_dev(seq_lens, "seq_lens", B)
+    if maps == 2:
+        import torch
+        f32 = (torch.float32,)
+        extra = (_dev(lam, "lam", f32, Hq // 2),
+                 None if norm_weight is None else _dev(norm_weight, "norm_weight", f32, 256),
+                 float(norm_eps))
+    dst = _dev(out, "out", T.out_types, rows * Hq * 128)
+    st = _stream(stream)
+    n = ctypes.c_size_t()
+    _check(size(h, *sizes, ctypes.byref(n)))
+    ws, p, nbytes = _scratch(n.value, workspace, st, q.device)
+    _check(fn(h, qp, qs, *starts, table, lens, *sizes, float(scale), *extra, dst, code, p, nbytes,
+              st))
+
+
+def _size_call(fn, *args):
+    n = ctypes.c_size_t()
+    _check(fn(*args, ctypes.byref(n)))
+    return n.value
+
+
+def paged_prompt_workspace(h, tokens, batch, num_q_heads, max_blocks):
+    return _size_call(_lib.ema_paged_prompt_workspace, h, tokens, batch, num_q_heads, max_blocks)
+
+
+def paged_diff_workspace(h, batch, num_q_heads, max_blocks):
+    return _size_call(_lib.ema_paged_diff_workspace, h, batch, num_q_heads, max_blocks)
+
+
+def paged_diff_prompt_workspace(h, tokens, batch, num_q_heads, max_blocks):
+    return _size_call(_lib.ema_paged_diff_prompt_workspace, h, tokens, batch, num_q_heads,
+                      max_blocks)
+
+
+def paged_prompt_attention(h, q, query_start, block_table, seq_lens, out, scale=0.0,
+                           workspace=None, stream=None):
+    """Causal attention of prompt chunks: q [T][Hq][128] (16-bit, tokens any multiple
+    of 8 elements apart), query_start int32 [B + 1], block_table int32
+    [B][max_blocks], seq_lens int32 [B], out [T][Hq][128] of float32, float16 or
+    bfloat16. Without ``workspace`` (a byte tensor of paged_prompt_workspace bytes)
+    the call takes one from torch's allocator."""
+    _attention_op(h, _lib.ema_paged_prompt_attention, _lib.ema_paged_prompt_workspace, 1, q,
+                  query_start, block_table, seq_lens, out, scale, None, None, 0.0, workspace,
+                  stream)
+
+
+def paged_diff_attention(h, q, block_table, seq_lens, lam, out, scale=0.0, norm_weight=None,
+                         norm_eps=0.0, workspace=None, stream=None):
+    """Differential attention of one token per sequence: q [B][Hq][128], lam float32
+    [Hq / 2], out [B][Hq / 2][256]; with norm_weight (float32 [256]) each output
+    row is divided by its root mean square and multiplied by it."""
+    _attention_op(h, _lib.ema_paged_diff_attention, _lib.ema_paged_diff_workspace, 2, q, None,
+                  block_table, seq_lens, out, scale, lam, norm_weight, norm_eps, workspace, stream)
+
+
+def paged_diff_prompt_attention(h, q, query_start, block_table, seq_lens, lam, out, scale=0.0,
+                                norm_weight=None, norm_eps=0.0, workspace=None, stream=None):
+    """Differential attention of prompt chunks: rows as in paged_prompt_attention,
+    heads, lam and norm as in paged_diff_attention; out [T][Hq / 2][256]."""
+    _attention_op(h, _lib.ema_paged_diff_prompt_attention, _lib.ema_paged_diff_prompt_workspace, 2,
+                  q, query_start, block_table, seq_lens, out, scale, lam, norm_weight, norm_eps,
+                  workspace, stream)
 
 
 # ---- slab management of the slice --------------------------------------------------
