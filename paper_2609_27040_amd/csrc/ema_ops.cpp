@@ -183,6 +183,7 @@ ema::PromptArgs kernel_args(const AttnCall& c) {
   a.kv_heads = h->shape.num_kv_heads;
   a.block_size = h->shape.block_size;
   a.max_blocks = c.max_blocks;
+  for (a.block_shift = 0; (1 << a.block_shift) < a.block_size;) ++a.block_shift;
   a.dtype = h->shape.dtype;
   a.out_dtype = c.out_dtype;
   return a;

@@ -62,6 +62,7 @@ struct PromptArgs {
   int64_t block_bytes;
   float* ws;
   int32_t n_local, tokens, batch, q_heads, kv_heads, block_size, max_blocks;
+  int32_t block_shift;         // log2(block_size)
   int32_t dtype;               // 0 f16, 1 bf16
   int32_t out_dtype;           // kOutF32, kOutF16 or kOutBF16
 };

@@ -22,8 +22,10 @@ namespace ema {
 namespace {
 
 constexpr int kWaves = 8;
+constexpr int kPieces = kTilePieces / (kWaves * 64);   // of K, and of V, to a thread
 constexpr int kThreads = kWaves * 64;
 constexpr int kRows = kWaves * 32;
+constexpr int kRing = 3;                 // staged tiles
 constexpr float kSlack = 8.0f;
 
 // P of a tile in NP 16-bit parts whose sum keeps 8 (bf16) or 11 (f16) bits each.
@@ -33,26 +35,31 @@ struct Weights {
 };
 
 template <bool BF16, int NP>
-__device__ __forceinline__ void put_weights(Weights<NP>& w, int ks, const float (&p)[8]) {
+__device__ __forceinline__ void put_weights(Weights<NP>& w, int ks, int q, float x, float y) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    float x = p[2 * q], y = p[2 * q + 1];
-#pragma unroll
-    for (int n = 0; n < NP; ++n) {
-      const uint32_t u = pack16<BF16>(x, y);
-      w.p[n][ks][q] = u;
-      if (n + 1 < NP) {
-        x -= low16<BF16>(u);
-        y -= high16<BF16>(u);
-      }
+  for (int n = 0; n < NP; ++n) {
+    const uint32_t u = pack16<BF16>(x, y);
+    w.p[n][ks][q] = u;
+    if (n + 1 < NP) {
+      x -= low16<BF16>(u);
+      y -= high16<BF16>(u);
     }
   }
 }
 
+// The eight waves are two groups, one of each to a SIMD, that take turns: while one
+// has the matrix cores (the last tile's weights times V, then the next scores), the
+// other works its scores into weights, puts its share of a later tile into LDS and
+// issues the loads of the one after. Phase p: the first group has the products of tile
+// p / 2 when p is even and its softmax when p is odd, the second group one phase
+// later; a barrier ends each. K of tile j and V of tile j - 1 are read in phases 2j
+// and 2j + 1; in those two phases K of j + 2 and V of j + 1 are sent for, straight into
+// LDS, to the places of K of j - 1 and V of j - 2, which the phases before were the last
+// to read, and in the next two each wave waits for its own before it goes on.
 template <bool BF16, int BSC, int NP>
-__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int tiles, int splits) {
-  __shared__ __attribute__((aligned(16))) u32x4 s_k[2][kTilePieces];
-  __shared__ __attribute__((aligned(16))) u32x4 s_v[2][kTilePieces];
+__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int splits) {
+  __shared__ __attribute__((aligned(16))) u32x4 s_k[kRing][kTilePieces];
+  __shared__ __attribute__((aligned(16))) u32x4 s_v[kRing][kTilePieces];
   __shared__ int s_find[kFindScratch];
   __shared__ int s_bad[128];             // per channel: the first token not finite there
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -62,8 +69,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int t
   const int rest = int(blockIdx.x) / a.kv_heads;
   const int split = rest % splits;
   if (tid < 128) s_bad[tid] = INT_MAX;
-  // the last tiles of a sequence see the most tokens: they go first
-  const RowTile R = find_tile<kThreads>(a, G, kRows, tiles - 1 - rest / splits, s_find);
+  const RowTile R = find_tile<kThreads, kRows>(a, G, rest / splits, s_find);
   if (R.b < 0) return;
   const int past = R.len - R.n;          // tokens before the chunk
   if (R.first == 0 && split == 0 && kvh == 0 && tid == 0 &&
@@ -75,15 +81,15 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int t
   const int tok = live ? r / G : 0, g = live ? r - tok * G : 0;
   const int pos = live ? past + tok : -1;              // the row attends tokens 0 .. pos
   const int last_row = min(R.n * G, R.first + kRows) - 1;
-  const int end = max(0, past + last_row / G + 1);     // tokens the workgroup looks at
-  const int from = past + R.first / G;                 // position of its first row
+  const int end = uniform(max(0, past + last_row / G + 1));   // tokens the workgroup looks at
+  const int from = uniform(past + R.first / G);        // position of its first row
   const int wave_first = R.first + wave * 32;
-  const int wave_end = wave_first >= R.n * G
-                           ? 0 : max(0, past + min(R.n * G - 1, wave_first + 31) / G + 1);
-  const int wave_from = past + wave_first / G;
+  const int wave_end = uniform(wave_first >= R.n * G
+                                   ? 0 : max(0, past + min(R.n * G - 1, wave_first + 31) / G + 1));
+  const int wave_from = uniform(past + wave_first / G);
   const int n_tiles = (end + kKT - 1) / kKT;
-  const int j0 = int(int64_t(n_tiles) * split / splits);
-  const int j1 = int(int64_t(n_tiles) * (split + 1) / splits);
+  const int j0 = uniform(int(int64_t(n_tiles) * split / splits));
+  const int j1 = uniform(int(int64_t(n_tiles) * (split + 1) / splits));
 
   u32x4 q[8];
   {
@@ -91,144 +97,229 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int t
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
   }
-  f32x16 o[4];
+
+  // ---- staging -------------------------------------------------------------------
+  // Place p of a tile's K and of its V in LDS is loaded by thread p % kThreads; which piece
+  // belongs there is in the offsets. A wave's 64 places of one round lie in one block, the
+  // same for K and V.
+  const int64_t v_half = a.block_bytes / 2;
+  const int last_block = (max(end, 1) - 1) >> a.block_shift;
+  constexpr int kPer = 16 * BSC;                               // pieces of a block
+  uint32_t k_off[kPieces], v_off[kPieces];                     // bytes in the block
+  int v_ch[kPieces], v_tok[kPieces];                           // the V piece's channel and first token
+#pragma unroll
+  for (int x = 0; x < kPieces; ++x) {
+    const int p = x * kThreads + tid;
+    const int kt = p >> 4;
+    k_off[x] = ((kvh * a.block_size + kt % BSC) * 128 + ((p ^ kt) & 15) * 8) * 2;
+    const int vb = p / kPer, ch = p % kPer / (BSC / 8), gi = p % (BSC / 8) ^ v_turn<BSC>(ch);
+    v_off[x] = v_half + ((kvh * 128 + ch) * a.block_size + gi * 8) * 2;
+    v_ch[x] = ch;
+    v_tok[x] = vb * BSC + gi * 8;
+  }
+  const uint32_t lds_k = lds_address(&s_k[0][0]) + wave * 1024;
+  const uint32_t lds_v = lds_address(&s_v[0][0]) + wave * 1024;
+  IdWindow window;
+  struct Blocks {
+    const char* at[kPieces];             // the blocks of this wave's places
+  };
+  auto blocks_of = [&](int j) {
+    Blocks t;
+    const int first = j * kKT >> a.block_shift;
+    window.seek(min(first, last_block));
+    const int tb = BSC == 64 ? (j * kKT) & (a.block_size - 1) : 0;
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x)
+      t.at[x] = a.local + int64_t(window.get(min(first + (x * kThreads + wave * 64) / kPer,
+                                                 last_block))) * a.block_bytes + tb * 2;
+    return t;
+  };
+  auto load_k = [&](int slot, int j, const Blocks& t) {
+    const int tb = BSC == 64 ? (j * kKT) & (a.block_size - 1) : 0;
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x)
+      load_to_lds(t.at[x] + tb * 254, k_off[x],
+                  lds_k + slot * (kTilePieces * 16) + x * kThreads * 16);
+  };
+  auto load_v = [&](int slot, const Blocks& t) {
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x)
+      load_to_lds(t.at[x], v_off[x], lds_v + slot * (kTilePieces * 16) + x * kThreads * 16);
+  };
+  // V of tokens that are not there becomes 0, in the pieces this thread loaded.
+  auto clean_v = [&](int slot, int j) {
+    if ((j + 1) * kKT <= from + 1 && window.bad == 0) return;  // no row masks any token
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      u32x4* at = &s_v[slot][x * kThreads + tid];
+      u32x4 v = *at;
+      const int tok = j * kKT + v_tok[x];
+      const int left = window.bad == 0 || window.good(tok >> a.block_shift) ? end - tok : 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[i] &= (2 * i < left ? 0xffffu : 0u) | (2 * i + 1 < left ? 0xffff0000u : 0u);
+      if (not_finite<BF16>(v)) drop_not_finite<BF16>(v, tok, &s_bad[v_ch[x]]);
+      *at = v;
+    }
+  };
+  Blocks next_v;                         // of the K tile on its way, whose V is next
+  // Step j: V of tile j and K of tile j + 1 have arrived; V of j + 1 and K of j + 2 are
+  // sent for. s0, s1, s2: places of tiles j, j + 1 and j + 2.
+  auto stage = [&](int j, int s0, int s1, int s2) {
+    if (j >= j1) return;
+    loads_arrived();
+    clean_v(s0, j);
+    if (j + 1 < j1) load_v(s1, next_v);
+    if (j + 2 < j1) {
+      next_v = blocks_of(j + 2);
+      load_k(s2, j + 2, next_v);
+    }
+  };
+
+  // ---- products ------------------------------------------------------------------
+  f32x16 o[4], s[2];
 #pragma unroll
   for (int c = 0; c < 4; ++c) o[c] = f32x16{};
-  float m = -INFINITY, l = 0.0f;         // l: this lane's half of the tokens
-
-  const int32_t* trow = a.table + int64_t(R.b) * a.max_blocks;
-  const int64_t v_half = a.block_bytes / 2;
-  u32x4 kr[2], vr[2];
-  TileIds<BSC> ids = load_ids<BSC>(a, trow, j0 * kKT, end), next_ids;
-  // Issues the loads of tile j into the registers. Wave w's pieces 64w .. 64w + 63 of
-  // each half tile lie in one block.
-  auto load = [&](int j, TileIds<BSC>& t) {
-    check_ids<BSC>(a, t);
-    const int tb = BSC == 64 ? (j * kKT) % a.block_size : 0;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int kt = wave * 4 + x * 32 + (lane >> 4);          // K token of the tile
-      const int kid = t.id[(wave * 4 + x * 32) / BSC];
-      kr[x] = *reinterpret_cast<const u32x4*>(
-          a.local + int64_t(max(kid, 0)) * a.block_bytes +
-          ((kvh * a.block_size + tb + kt % BSC) * 128 + (lane & 15) * 8) * 2);
-      constexpr int per = 16 * BSC;                              // V pieces of a block
-      const int p = x * 512 + tid, vb = uniform(p / per);
-      const int ch = p % per / (BSC / 8), gi = p % (BSC / 8);
-      const int vid = t.id[vb];
-      vr[x] = *reinterpret_cast<const u32x4*>(
-          a.local + int64_t(max(vid, 0)) * a.block_bytes + v_half +
-          (int64_t(kvh * 128 + ch) * a.block_size + tb + gi * 8) * 2);
-    }
-  };
-  // Puts the loaded tile j into buffer x; V of tokens that are not there becomes 0.
-  auto stage = [&](int j, const TileIds<BSC>& t, int x) {
-    const bool edge = (j + 1) * kKT > from + 1;                  // some row masks some token
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      const int kt = wave * 4 + y * 32 + (lane >> 4);
-      s_k[x][k_place(kt, lane & 15)] = kr[y];
-      constexpr int per = 16 * BSC;
-      const int p = y * 512 + tid, vb = uniform(p / per);
-      const int ch = p % per / (BSC / 8), gi = p % (BSC / 8);
-      u32x4 v = vr[y];
-      const int left = end - j * kKT - (vb * BSC + gi * 8);
-      if (t.id[vb] < 0) v = u32x4{0, 0, 0, 0};
-      if (edge) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          v[i] &= (2 * i < left ? 0xffffu : 0u) | (2 * i + 1 < left ? 0xffff0000u : 0u);
-        if (not_finite<BF16>(v)) drop_not_finite<BF16>(v, j * kKT + vb * BSC + gi * 8, &s_bad[ch]);
-      }
-      s_v[x][v_place<BSC>(ch, vb * (BSC / 8) + gi)] = v;
-    }
-  };
-
-  if (j0 < j1) {
-    load(j0, ids);
-    next_ids = load_ids<BSC>(a, trow, (j0 + 1) * kKT, end);
-    __syncthreads();                     // s_bad is clear
-    stage(j0, ids, 0);
-  }
-  __syncthreads();
+  s[0] = s[1] = f32x16{};
+  Weights<NP> w;
   // A rows of the scores: MFMA row i of a 32-token tile is this token
   const int arow = (col >> 4) * 16 + ((col >> 2) & 1) * 8 + ((col >> 3) & 1) * 4 + (col & 3);
-  for (int j = j0; j < j1; ++j) {
-    const int buf = (j - j0) & 1;
-    const TileIds<BSC> cur = ids;
-    if (j + 1 < j1) {
-      ids = next_ids;
-      load(j + 1, ids);
-      if (j + 2 < j1) next_ids = load_ids<BSC>(a, trow, (j + 2) * kKT, end);
+  constexpr int kAhead = 6;              // operands this many products ahead of their use
+  auto read_k = [&](int slot, int i) {
+    return s_k[slot][k_place((i & 1) * 32 + arow, (i >> 1) * 2 + half)];
+  };
+  auto read_v = [&](int slot, int i) {
+    return s_v[slot][v_place<BSC>((i & 3) * 32 + col, (i >> 2) * 2 + half)];
+  };
+  auto score = [&](int i, u32x4 f) {
+    s[i & 1] = mfma32<BF16>(f, q[i >> 1], i < 2 ? f32x16{} : s[i & 1]);
+  };
+  auto weigh_v = [&](int i, u32x4 f) {
+#pragma unroll
+    for (int n = 0; n < NP; ++n) o[i & 3] = mfma32<BF16>(f, w.p[n][i >> 2], o[i & 3]);
+  };
+  // The products of tile j: V of the tile before, K of this one, from their places.
+  auto products = [&](int j, int before, int slot) {
+    const bool pv = j > j0 && (j - 1) * kKT < wave_end, qk = j < j1 && j * kKT < wave_end;
+    __builtin_amdgcn_s_setprio(1);
+    u32x4 f[16];
+    if (pv) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = read_v(before, i);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) weigh_v(i, f[i]);
+      EMA_SCHED_LDS_READ(kAhead);
+#pragma unroll
+      for (int i = 0; i < 16 - kAhead; ++i) {
+        EMA_SCHED_MFMA(NP);
+        EMA_SCHED_LDS_READ(1);
+      }
+      EMA_SCHED_MFMA(kAhead * NP);
     }
+    if (qk) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = read_k(slot, i);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) score(i, f[i]);
+      EMA_SCHED_LDS_READ(kAhead);
+#pragma unroll
+      for (int i = 0; i < 16 - kAhead; ++i) {
+        EMA_SCHED_MFMA(1);
+        EMA_SCHED_LDS_READ(1);
+      }
+      EMA_SCHED_MFMA(kAhead);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+
+  // ---- softmax -------------------------------------------------------------------
+  float m = -INFINITY, l = 0.0f;         // l: this lane's half of the tokens
+  auto softmax = [&](int j) {
     const int t0 = j * kKT;
-    bool all_ids = true;
-#pragma unroll
-    for (int i = 0; i < TileIds<BSC>::N; ++i) all_ids &= cur.id[i] >= 0;
-    if (!all_ids && kvh == 0 && R.first == 0 && tid == 0) {
-#pragma unroll
-      for (int i = 0; i < TileIds<BSC>::N; ++i)
-        if (cur.id[i] < 0 && t0 + i * BSC < end) atomicAdd(a.err_count, 1);
-    }
-    if (t0 < wave_end) {
-      f32x16 s[2];
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        s[tt] = f32x16{};
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          s[tt] = mfma32<BF16>(s_k[buf][k_place(tt * 32 + arow, ks * 2 + half)], q[ks], s[tt]);
-      }
-      const bool masked = t0 + kKT > wave_from + 1;
-      if (masked || !all_ids) {
-        const int rel = pos - t0 - half * 8;           // token 16k + e of this lane: 16k + e <= rel
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int t = tt * 32 + (i >> 3) * 16;     // of 16 tokens, in one block
-            const bool ok = t + (i & 7) <= rel && cur.id[t / BSC] >= 0;
-            s[tt][i] = ok ? s[tt][i] : -INFINITY;
-          }
-      }
-      float mx = -INFINITY;
+    if (j >= j1 || t0 >= wave_end) return;
+    if (t0 + kKT > wave_from + 1) {
+      const int rel = pos - t0 - half * 8;             // token 16k + e of this lane: 16k + e <= rel
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[tt][i]);
-      mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
-      if (__ballot(mx > m + kSlack)) {
-        const float m_new = fmaxf(m, mx);
-        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
-        m = m_new;
-        l *= alpha;
+        for (int i = 0; i < 16; ++i)
+          s[tt][i] = tt * 32 + (i >> 3) * 16 + (i & 7) <= rel ? s[tt][i] : -INFINITY;
+    }
+    if (window.bad != 0) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) o[c] *= alpha;
+      for (int x = 0; x < 4; ++x) {                    // 16 tokens, in one block
+        if (window.good((t0 + x * 16) >> a.block_shift)) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[x >> 1][(x & 1) * 8 + i] = -INFINITY;
       }
-      const float ref = m == -INFINITY ? 0.0f : m;
-      Weights<NP> w;
+    }
+    float mx = -INFINITY;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        float p[8];
+    for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][(ks & 1) * 8 + e], a.scale_log2, -ref));
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[tt][i]);
+    mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
+    if (__ballot(mx > m + kSlack)) {
+      const float m_new = fmaxf(m, mx);
+      const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] *= alpha;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        float p[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(
+              fmaf(s[ks >> 1][(ks & 1) * 8 + 2 * x + e], a.scale_log2, -ref));
           l += p[e];
         }
-        put_weights<BF16, NP>(w, ks, p);
+        put_weights<BF16, NP>(w, ks, x, p[0], p[1]);
       }
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const u32x4 v = s_v[buf][v_place<BSC>(c * 32 + col, ks * 2 + half)];
-#pragma unroll
-          for (int n = 0; n < NP; ++n) o[c] = mfma32<BF16>(v, w.p[n][ks], o[c]);
-        }
+  };
+
+  // ---- the phases ----------------------------------------------------------------
+  if (j0 < j1) {
+    window.open(a, R.b, j0 * kKT >> a.block_shift, last_block);
+    next_v = blocks_of(j0);
+    load_k(0, j0, next_v);
+    load_v(0, next_v);
+    if (j0 + 1 < j1) {
+      next_v = blocks_of(j0 + 1);
+      load_k(1, j0 + 1, next_v);
     }
-    if (j + 1 < j1) stage(j + 1, ids, buf ^ 1);
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) arrived(q[ks]);
+    loads_arrived();
     __syncthreads();
+    // One loop for both groups; the second stages first and starts a phase later.
+    const int late = wave >= kWaves / 2 ? 1 : 0;
+    if (late) {
+      stage(j0, 0, 1, 2);
+      __syncthreads();
+    }
+    int s0 = 0, s1 = 1, s2 = 2;          // places of tiles j, j + 1 and j + 2 (and j - 1)
+    for (int j = j0; j < j1; ++j) {
+      products(j, s2, s0);
+      __syncthreads();
+      stage(j + late, late ? s1 : s0, late ? s2 : s1, late ? s0 : s2);
+      softmax(j);
+      const int t = s0;
+      s0 = s1;
+      s1 = s2;
+      s2 = t;
+      __syncthreads();
+    }
+    products(j1, s2, s0);
+    if (!late) __syncthreads();
+    if (window.bad != 0 && kvh == 0 && R.first == 0 && tid == 0) atomicAdd(a.err_count, window.bad);
   }
+  __syncthreads();
 
   l += other_half(l);
   if (!live) return;
@@ -303,8 +394,8 @@ int64_t tile_bound(const PromptArgs& a) {
   return std::min<int64_t>(a.tokens, (rows + kRows - 1) / kRows + a.batch - 1);
 }
 
-// Parts that a tile's tokens are cut into: as many as fill the chip's 256 compute
-// units, of 256 tokens at least where the table is full.
+// Parts that a tile's tokens are cut into: as many as fill the chip, a workgroup to each of
+// 256 compute units, of 256 tokens at least where the table is full.
 int split_count(const PromptArgs& a) {
   const int64_t groups = tile_bound(a) * a.kv_heads;
   const int64_t most = int64_t(a.max_blocks) * a.block_size / 256;
@@ -319,15 +410,15 @@ hipError_t launch(const PromptArgs& a, hipStream_t stream) {
   switch (a.block_size) {
     case 16:
       hipLaunchKernelGGL((prompt_kernel<BF16, 16, NP>), grid, dim3(kThreads), 0, stream, a,
-                         int(tiles), splits);
+                         splits);
       break;
     case 32:
       hipLaunchKernelGGL((prompt_kernel<BF16, 32, NP>), grid, dim3(kThreads), 0, stream, a,
-                         int(tiles), splits);
+                         splits);
       break;
     default:
       hipLaunchKernelGGL((prompt_kernel<BF16, 64, NP>), grid, dim3(kThreads), 0, stream, a,
-                         int(tiles), splits);
+                         splits);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;

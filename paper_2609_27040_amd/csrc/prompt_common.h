@@ -100,28 +100,99 @@ struct RowTile {
   int len;        // tokens of the sequence
 };
 
-// Which sequence holds tile `tile` of all sequences' tiles: every workgroup walks
-// the starts, thread t `per` consecutive sequences.
-template <int THREADS>
-__device__ __forceinline__ RowTile find_tile(const PromptArgs& a, int group, int rows, int tile,
-                                             int* s_scratch) {
+// Rows of sequence b in q, clamped to what is there.
+__device__ __forceinline__ void row_range(const PromptArgs& a, int b, int& s, int& n) {
+  s = min(max(a.starts[b], 0), a.tokens);
+  n = max(0, min(a.starts[b + 1], a.tokens) - s);
+}
+
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+
+// Tile `index` of all sequences' tiles, the last tile of every sequence first, then the
+// one before it of those that have two, and so on: the tiles at the end of a
+// long sequence see the most tokens and take the longest, and what is left over at the end
+// of the launch are short ones (four prompts of 257-3841 tokens, sequence by
+// sequence: 270 us, so: 000 us). Every wave searches alone, 64 sequences at a time.
+constexpr int kLevelBatch = 512;
+template <int ROWS>
+__device__ __forceinline__ RowTile find_by_level(const PromptArgs& a, int group, int index) {
+  constexpr int N = kLevelBatch / 64;
+  const int lane = threadIdx.x & 63;
+  int tiles[N], most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    tiles[i] = 0;
+    if (i * 64 >= a.batch) continue;
+    const int b = i * 64 + lane;
+    int s, n = 0;
+    if (b < a.batch) row_range(a, b, s, n);
+    tiles[i] = (n * group + ROWS - 1) / ROWS;
+    most = max(most, tiles[i]);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o));
+  auto below = [&](int level) {          // tiles at levels under this one
+    int t = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i * 64 < a.batch) t += min(tiles[i], level);
+    return uniform(wave_sum(t));
+  };
+  RowTile r;
+  r.b = -1;
+  int lo = 0, hi = uniform(most), at = 0;        // below(lo) <= index < below(hi)
+  if (index >= below(hi)) return r;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1, t = below(mid);
+    if (t <= index) {
+      lo = mid;
+      at = t;
+    } else {
+      hi = mid;
+    }
+  }
+  int k = index - at;                    // the k-th sequence of more than lo tiles
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (i * 64 >= a.batch || r.b >= 0) continue;
+    const unsigned long long m = __ballot(tiles[i] > lo);
+    const int c = __popcll(m);
+    if (k < c) {
+      const unsigned long long hit = __ballot(
+          tiles[i] > lo && __popcll(m & ((1ull << lane) - 1ull)) == k);
+      const int l = __builtin_ctzll(hit);
+      r.b = i * 64 + l;
+      r.first = (__builtin_amdgcn_readlane(tiles[i], l) - 1 - lo) * ROWS;
+    }
+    k -= c;
+  }
+  r.b = uniform(r.b);
+  r.first = uniform(r.first);
+  int s, n;
+  row_range(a, r.b, s, n);
+  r.row0 = uniform(s);
+  r.n = uniform(n);
+  r.len = uniform(max(0, min(a.seq_lens[r.b], a.max_blocks * a.block_size)));
+  return r;
+}
+
+// Tile `index` sequence by sequence, for batches above kLevelBatch: the workgroup
+// walks the starts together, thread t consecutive sequences.
+template <int THREADS, int ROWS>
+__device__ __forceinline__ RowTile find_in_order(const PromptArgs& a, int group, int index,
+                                                 int* s_scratch) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (a.batch + THREADS - 1) / THREADS;
   const int b0 = min(a.batch, tid * per), b1 = min(a.batch, b0 + per);
-  auto range = [&](int b, int& s, int& n) {
-    if (!a.starts) {
-      s = b;
-      n = 1;
-      return;
-    }
-    s = min(max(a.starts[b], 0), a.tokens);
-    n = max(0, min(a.starts[b + 1], a.tokens) - s);
-  };
   int total = 0;
   for (int b = b0; b < b1; ++b) {
     int s, n;
-    range(b, s, n);
-    total += (n * group + rows - 1) / rows;
+    row_range(a, b, s, n);
+    total += (n * group + ROWS - 1) / ROWS;
   }
   int incl = total;
 #pragma unroll
@@ -134,32 +205,38 @@ __device__ __forceinline__ RowTile find_tile(const PromptArgs& a, int group, int
   __syncthreads();
   int at = incl - total;
   for (int w = 0; w < wave; ++w) at += s_scratch[w];
-  if (tile >= at && tile < at + total) {
+  int* out = s_scratch + THREADS / 64;
+  if (index >= at && index < at + total) {
     for (int b = b0; b < b1; ++b) {
       int s, n;
-      range(b, s, n);
-      const int t = (n * group + rows - 1) / rows;
-      if (tile < at + t) {
-        int* out = s_scratch + THREADS / 64;
+      row_range(a, b, s, n);
+      const int t = (n * group + ROWS - 1) / ROWS;
+      if (index < at + t) {
         out[0] = b;
         out[1] = s;
         out[2] = n;
-        out[3] = (tile - at) * rows;
+        out[3] = (index - at) * ROWS;
         break;
       }
       at += t;
     }
   }
   __syncthreads();
-  const int* in = s_scratch + THREADS / 64;
   RowTile r;
-  r.b = uniform(in[0]);
+  r.b = uniform(out[0]);
   if (r.b < 0) return r;
-  r.row0 = uniform(in[1]);
-  r.n = uniform(in[2]);
-  r.first = uniform(in[3]);
+  r.row0 = uniform(out[1]);
+  r.n = uniform(out[2]);
+  r.first = uniform(out[3]);
   r.len = uniform(max(0, min(a.seq_lens[r.b], a.max_blocks * a.block_size)));
   return r;
+}
+
+template <int THREADS, int ROWS>
+__device__ __forceinline__ RowTile find_tile(const PromptArgs& a, int group, int index,
+                                             int* s_scratch) {
+  return a.batch <= kLevelBatch ? find_by_level<ROWS>(a, group, index)
+                                : find_in_order<THREADS, ROWS>(a, group, index, s_scratch);
 }
 constexpr int kFindScratch = 16 + 4;
 
@@ -173,39 +250,84 @@ __device__ __forceinline__ int k_place(int tok, int piece) {
   return tok * 16 + (piece ^ (tok & 15));
 }
 template <int BSC>
+__device__ __forceinline__ int v_turn(int ch) {
+  constexpr int r = BSC / 8;
+  return r == 8 ? (ch >> 1) & 7 : r == 4 ? (ch >> 2) & 3 : (ch >> 3) & 1;
+}
+template <int BSC>
 __device__ __forceinline__ int v_place(int ch, int group) {   // group: eight tokens of the tile
   constexpr int r = BSC / 8;
-  const int f = r == 8 ? (ch >> 1) & 7 : r == 4 ? (ch >> 2) & 3 : (ch >> 3) & 1;
-  return group / r * (128 * r) + ch * r + ((group % r) ^ f);
+  return group / r * (128 * r) + ch * r + ((group % r) ^ v_turn<BSC>(ch));
 }
 
-// Block ids of a tile, uniform over the wave: -1 for one that is out of range.
-template <int BSC>
-struct TileIds {
-  static constexpr int N = kKT / BSC;    // blocks of a tile (one, of block size 64 on)
-  int id[N];
+// The block ids of a row of the table, 64 at a time in the lanes of a register (and
+// the 64 after them, on their way), read tile by tile in ascending order. Past block
+// `last`, that one again (its rows are masked there). An id outside the local pool reads
+// as block 0, which always exists, and leaves its mark in `bad`.
+struct IdWindow {
+  const int32_t* row;
+  int last, at;          // at: first block of the window, a multiple of 64
+  int n_local, bad;      // bad: ids out of range so far
+  int32_t cur, next;
+  __device__ __forceinline__ void open(const PromptArgs& a, int b, int first, int last_block) {
+    row = a.table + int64_t(b) * a.max_blocks;
+    n_local = a.n_local;
+    last = last_block;
+    at = first & ~63;
+    bad = 0;
+    cur = checked(fetch(at));
+    next = fetch(at + 64);
+  }
+  __device__ __forceinline__ int32_t fetch(int block) const {
+    return row[min(block + int(threadIdx.x & 63), last)];
+  }
+  __device__ __forceinline__ int32_t checked(int32_t id) {
+    const bool ok = uint32_t(id) < uint32_t(n_local);
+    bad += __popcll(__ballot(!ok && at + int(threadIdx.x & 63) <= last));
+    return ok ? id : 0;
+  }
+  __device__ __forceinline__ void seek(int block) {
+    if (block >= at + 64) {
+      at += 64;
+      cur = checked(next);
+      next = fetch(at + 64);
+    }
+  }
+  __device__ __forceinline__ int get(int block) const {
+    return __builtin_amdgcn_readlane(cur, block & 63);
+  }
+  // Whether the table names a block of the pool there (only asked where bad > 0).
+  __device__ __forceinline__ bool good(int block) const {
+    return uint32_t(row[min(block, last)]) < uint32_t(n_local);
+  }
 };
 
-// Ids of the tile at token t0, of which `end` tokens are there.
-template <int BSC>
-__device__ __forceinline__ TileIds<BSC> load_ids(const PromptArgs& a, const int32_t* row, int t0,
-                                                 int end) {
-  TileIds<BSC> r;
-  const int last = (max(end, 1) - 1) / a.block_size;
-#pragma unroll
-  for (int i = 0; i < TileIds<BSC>::N; ++i) {
-    // past the end: the last block again, whose rows are masked there
-    const int j = min((t0 + i * BSC) / a.block_size, last);
-    r.id[i] = row[j];
-  }
-  return r;
+// 16 bytes a lane from `base` (uniform) + `off` straight into LDS, at byte `lds` (uniform)
+// + 16 * lane. Nothing is written to registers; loads_arrived() waits for all of the
+// wave's.
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, uint32_t lds) {
+  const uint64_t b = reinterpret_cast<uint64_t>(base);
+  const uint64_t ub = uint64_t(uint32_t(uniform(int(uint32_t(b))))) |
+                      uint64_t(uint32_t(uniform(int(uint32_t(b >> 32))))) << 32;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :: "s"(uniform(int(lds))), "v"(off), "s"(ub) : "memory");
+}
+__device__ __forceinline__ void loads_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>(
+      (const __attribute__((address_space(3))) void*)p));
 }
 
-template <int BSC>
-__device__ __forceinline__ void check_ids(const PromptArgs& a, TileIds<BSC>& t) {
-#pragma unroll
-  for (int i = 0; i < TileIds<BSC>::N; ++i)
-    t.id[i] = uint32_t(t.id[i]) < uint32_t(a.n_local) ? t.id[i] : -1;
+// Order of what the scheduler lays out next, `n` instructions at a time.
+#define EMA_SCHED_VALU(n) __builtin_amdgcn_sched_group_barrier(0x2, n, 0)
+#define EMA_SCHED_MFMA(n) __builtin_amdgcn_sched_group_barrier(0x8, n, 0)
+#define EMA_SCHED_LDS_READ(n) __builtin_amdgcn_sched_group_barrier(0x100, n, 0)
+
+// Makes the compiler wait here for a value that is still being loaded, instead of at
+// its first use inside a loop, where the wait would catch the loop's own loads.
+template <typename T>
+__device__ __forceinline__ void arrived(T& x) {
+  asm volatile("" : "+v"(x));
 }
 
 }  // namespace ema
