@@ -61,19 +61,19 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
   __shared__ __attribute__((aligned(16))) u32x4 s_k[kRing][kTilePieces];
   __shared__ __attribute__((aligned(16))) u32x4 s_v[kRing][kTilePieces];
   __shared__ int s_find[kFindScratch];
-  __shared__ int s_bad[128];             // per channel: the first token not finite there
+  __shared__ int s_bad[129];             // the first token not finite, per channel and of all
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int G = a.q_heads / a.kv_heads;
   const int kvh = int(blockIdx.x) % a.kv_heads;
   const int rest = int(blockIdx.x) / a.kv_heads;
   const int split = rest % splits;
-  if (tid < 128) s_bad[tid] = INT_MAX;
+  if (tid < 129) s_bad[tid] = INT_MAX;
   const RowTile R = find_tile<kThreads, kRows>(a, G, rest / splits, s_find);
   if (R.b < 0) return;
   const int past = R.len - R.n;          // tokens before the chunk
   if (R.first == 0 && split == 0 && kvh == 0 && tid == 0 &&
-      (past < 0 || R.len != a.seq_lens[R.b]))
+      (past < 0 || R.len != R.given))
     atomicAdd(a.err_count, 1);
 
   const int r = R.first + wave * 32 + col;
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         v[i] &= (2 * i < left ? 0xffffu : 0u) | (2 * i + 1 < left ? 0xffff0000u : 0u);
-      if (not_finite<BF16>(v)) drop_not_finite<BF16>(v, tok, &s_bad[v_ch[x]]);
+      if (not_finite<BF16>(v)) drop_not_finite<BF16>(v, tok, &s_bad[v_ch[x]], &s_bad[128]);
       *at = v;
     }
   };
@@ -184,7 +184,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
   Weights<NP> w;
   // A rows of the scores: MFMA row i of a 32-token tile is this token
   const int arow = (col >> 4) * 16 + ((col >> 2) & 1) * 8 + ((col >> 3) & 1) * 4 + (col & 3);
-  constexpr int kAhead = 6;              // operands this many products ahead of their use
+  // operands this many products ahead of their use (fewer where registers are short)
+  constexpr int kAhead = NP == 3 ? 4 : 6;
   auto read_k = [&](int slot, int i) {
     return s_k[slot][k_place((i & 1) * 32 + arow, (i >> 1) * 2 + half)];
   };
@@ -202,26 +203,29 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
   auto products = [&](int j, int before, int slot) {
     const bool pv = j > j0 && (j - 1) * kKT < wave_end, qk = j < j1 && j * kKT < wave_end;
     __builtin_amdgcn_s_setprio(1);
-    u32x4 f[16];
+    u32x4 f[16], g[kAhead];
     if (pv) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) f[i] = read_v(before, i);
 #pragma unroll
+      for (int i = 0; i < kAhead; ++i) g[i] = read_k(slot, i);   // not used where !qk
+#pragma unroll
       for (int i = 0; i < 16; ++i) weigh_v(i, f[i]);
       EMA_SCHED_LDS_READ(kAhead);
 #pragma unroll
-      for (int i = 0; i < 16 - kAhead; ++i) {
+      for (int i = 0; i < 16; ++i) {
         EMA_SCHED_MFMA(NP);
         EMA_SCHED_LDS_READ(1);
       }
-      EMA_SCHED_MFMA(kAhead * NP);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) g[i] = read_k(slot, i);
     }
     if (qk) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) f[i] = read_k(slot, i);
+      for (int i = 0; i < 16; ++i) f[i] = i < kAhead ? g[i] : read_k(slot, i);
 #pragma unroll
       for (int i = 0; i < 16; ++i) score(i, f[i]);
-      EMA_SCHED_LDS_READ(kAhead);
 #pragma unroll
       for (int i = 0; i < 16 - kAhead; ++i) {
         EMA_SCHED_MFMA(1);
@@ -323,11 +327,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
 
   l += other_half(l);
   if (!live) return;
+  if (s_bad[128] != INT_MAX)
 #pragma unroll
-  for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < 4; ++c)
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (pos >= s_bad[c * 32 + (i >> 2) * 8 + half * 4 + (i & 3)]) o[c][i] = NAN;
+      for (int i = 0; i < 16; ++i)
+        if (pos >= s_bad[c * 32 + (i >> 2) * 8 + half * 4 + (i & 3)]) o[c][i] = NAN;
   const int64_t orow = int64_t(R.row0 + tok) * a.q_heads + kvh * G + g;
   if (splits > 1) {
     const int64_t part = int64_t(split) * a.tokens * a.q_heads + orow;

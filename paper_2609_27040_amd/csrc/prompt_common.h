@@ -75,8 +75,9 @@ __device__ __forceinline__ bool not_finite(u32x4 v) {
 // part, 0 times them would be NaN for rows that do not attend them; the rows that do
 // get NaN at the end instead.
 template <bool BF16>
-__device__ __forceinline__ void drop_not_finite(u32x4& v, int tok, int* first) {
+__device__ __forceinline__ void drop_not_finite(u32x4& v, int tok, int* first, int* any) {
   constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u;
+  atomicMin(any, tok);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if ((v[i] & kExp) == kExp) {
@@ -98,6 +99,7 @@ struct RowTile {
   int n;          // its rows (tokens)
   int first;      // first (token, head) pair of the tile
   int len;        // tokens of the sequence
+  int given;      // its length as it is given
 };
 
 // Rows of sequence b in q, clamped to what is there.
@@ -106,46 +108,61 @@ __device__ __forceinline__ void row_range(const PromptArgs& a, int b, int& s, in
   n = max(0, min(a.starts[b + 1], a.tokens) - s);
 }
 
+// Sum and maximum (of values >= 0) over the wave's 64 lanes, uniform: DPP moves within
+// rows of 16 lanes, the row totals carried over to the last lane.
+template <typename Op>
+__device__ __forceinline__ int wave_reduce(int x, Op&& op) {
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));    // row_shr 1, 2, 4, 8
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));   // lane 15 of rows 0, 2 to 1, 3
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));   // lane 31 to rows 2, 3
+  return __builtin_amdgcn_readlane(x, 63);
+}
 __device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+  return wave_reduce(x, [](int p, int q) { return p + q; });
+}
+__device__ __forceinline__ int wave_max(int x) {
+  return wave_reduce(x, [](int p, int q) { return max(p, q); });
 }
 
 // Tile `index` of all sequences' tiles, the last tile of every sequence first, then the
 // one before it of those that have two, and so on: the tiles at the end of a
 // long sequence see the most tokens and take the longest, and what is left over at the end
 // of the launch are short ones (four prompts of 257-3841 tokens, sequence by
-// sequence: 270 us, so: 000 us). Every wave searches alone, 64 sequences at a time.
+// sequence: 246-270 us by their order, so: 240 us). Every wave searches alone, 64 sequences at a time.
 constexpr int kLevelBatch = 512;
 template <int ROWS>
 __device__ __forceinline__ RowTile find_by_level(const PromptArgs& a, int group, int index) {
   constexpr int N = kLevelBatch / 64;
   const int lane = threadIdx.x & 63;
-  int tiles[N], most = 0;
+  int tiles[N], start[N], rows[N], len[N];   // of sequences 64 * i + lane
+  int total = 0, most = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    tiles[i] = 0;
+    tiles[i] = rows[i] = start[i] = len[i] = 0;
     if (i * 64 >= a.batch) continue;
     const int b = i * 64 + lane;
-    int s, n = 0;
-    if (b < a.batch) row_range(a, b, s, n);
-    tiles[i] = (n * group + ROWS - 1) / ROWS;
+    if (b < a.batch) {
+      row_range(a, b, start[i], rows[i]);
+      len[i] = a.seq_lens[b];
+    }
+    tiles[i] = (rows[i] * group + ROWS - 1) / ROWS;
+    total += tiles[i];
     most = max(most, tiles[i]);
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o));
+  RowTile r;
+  r.b = -1;
+  if (index >= wave_sum(total)) return r;
   auto below = [&](int level) {          // tiles at levels under this one
     int t = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i)
       if (i * 64 < a.batch) t += min(tiles[i], level);
-    return uniform(wave_sum(t));
+    return wave_sum(t);
   };
-  RowTile r;
-  r.b = -1;
-  int lo = 0, hi = uniform(most), at = 0;        // below(lo) <= index < below(hi)
-  if (index >= below(hi)) return r;
+  int lo = 0, hi = wave_max(most), at = 0;     // below(lo) <= index < below(hi)
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1, t = below(mid);
     if (t <= index) {
@@ -167,16 +184,18 @@ __device__ __forceinline__ RowTile find_by_level(const PromptArgs& a, int group,
       const int l = __builtin_ctzll(hit);
       r.b = i * 64 + l;
       r.first = (__builtin_amdgcn_readlane(tiles[i], l) - 1 - lo) * ROWS;
+      r.row0 = __builtin_amdgcn_readlane(start[i], l);
+      r.n = __builtin_amdgcn_readlane(rows[i], l);
+      r.len = __builtin_amdgcn_readlane(len[i], l);
     }
     k -= c;
   }
   r.b = uniform(r.b);
   r.first = uniform(r.first);
-  int s, n;
-  row_range(a, r.b, s, n);
-  r.row0 = uniform(s);
-  r.n = uniform(n);
-  r.len = uniform(max(0, min(a.seq_lens[r.b], a.max_blocks * a.block_size)));
+  r.row0 = uniform(r.row0);
+  r.n = uniform(r.n);
+  r.given = uniform(r.len);
+  r.len = max(0, min(r.given, a.max_blocks * a.block_size));
   return r;
 }
 
@@ -228,7 +247,8 @@ __device__ __forceinline__ RowTile find_in_order(const PromptArgs& a, int group,
   r.row0 = uniform(out[1]);
   r.n = uniform(out[2]);
   r.first = uniform(out[3]);
-  r.len = uniform(max(0, min(a.seq_lens[r.b], a.max_blocks * a.block_size)));
+  r.given = uniform(a.seq_lens[r.b]);
+  r.len = max(0, min(r.given, a.max_blocks * a.block_size));
   return r;
 }
 
