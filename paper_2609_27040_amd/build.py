@@ -22,7 +22,8 @@ LIB = os.path.join(LIBDIR, "libema_slice.so")
 
 SOURCES = ["slice_book.cpp", "slab_book.cpp", "ema_slice.cpp", "slice_sched.cpp", "block_copy.hip",
            "paged_attention_mfma.hip", "attn_combine.hip", "ema_ops.cpp", "kv_tables.hip",
-           "kv_store.hip", "prompt_attention.hip", "diff_attention.hip"]
+           "kv_store.hip", "prompt_attention.hip", "diff_attention.hip",
+           "diff_prompt.hip"]
 CALIB_LIB = os.path.join(LIBDIR, "libema_calib.so")
 CALIB_SOURCES = ["hbm_calib.hip"]
 

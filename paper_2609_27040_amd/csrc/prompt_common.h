@@ -287,7 +287,7 @@ __device__ __forceinline__ int v_place(int ch, int group) {   // group: eight to
 struct IdWindow {
   const int32_t* row;
   int last, at;          // at: first block of the window, a multiple of 64
-  int n_local, bad;      // bad: ids out of range so far
+  int n_local = 0, bad = 0;      // bad: ids out of range so far
   int32_t cur, next;
   __device__ __forceinline__ void open(const PromptArgs& a, int b, int first, int last_block) {
     row = a.table + int64_t(b) * a.max_blocks;
@@ -332,6 +332,22 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, uint
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :: "s"(uniform(int(lds))), "v"(off), "s"(ub) : "memory");
 }
+// The same from an address per lane; NT: streamed past the caches.
+template <bool NT>
+__device__ __forceinline__ void load_lane_to_lds(const char* p, uint32_t lds) {
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
+                 :: "s"(uniform(int(lds))), "v"(p) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(uniform(int(lds))), "v"(p) : "memory");
+}
+// All of the wave's loads but the newest 16 have arrived.
+__device__ __forceinline__ void loads_arrived_but_16() {
+  asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+}
+// Nothing of the wave still reads LDS.
+__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ void loads_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return uint32_t(reinterpret_cast<uintptr_t>(
