@@ -145,8 +145,8 @@ int ema_paged_prompt_attention(ema_slice_t h, const void* q, int64_t q_stride,
  *              - lambda[i] * softmax_t(scale * q[2i + 1] . K[2j + 1]_t)) V[j]_t
  *   out[b][i] = o, or, with norm_weight, o / sqrt(mean(o^2) + norm_eps) * norm_weight
  * for t < seq_lens[b]. lambda: device float [num_q_heads / 2]; norm_weight:
- * device float [2 * head_dim] or NULL (a constant factor of the layer is folded
- * into it). out: device [batch][num_q_heads / 2][2 * head_dim] of out_dtype,
+ * device float [2 * head_dim], 16-byte aligned, or NULL (a constant factor of the
+ * layer is folded into it). out: device [batch][num_q_heads / 2][2 * head_dim] of out_dtype,
  * 16-byte aligned. q as for ema_paged_prompt_attention (row b is sequence b's);
  * block_table, seq_lens, scale as for ema_paged_decode_attention; length 0 gives zeros.
  * num_kv_heads must be even, num_q_heads / num_kv_heads a whole number. Async on

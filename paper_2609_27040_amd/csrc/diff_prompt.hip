@@ -1,141 +1,537 @@
-// Attention of prompt chunks and differential attention over the paged cache:
-// one wavefront per query row and output head, tokens over the lanes for the
-// scores, channels over the lanes for the output, in 32 bits throughout.
-#include "op_kernels.h"
-#include "attn_store.h"
+// Differential attention of prompt chunks over the paged cache, on the matrix cores, in
+// two launches.
+//
+// The maps' difference is smaller than the maps, so it is formed in 32 bits before anything
+// is rounded: the first launch finds each row's maximum m and sum l for each map (scores
+// only), the second computes the scores again and multiplies
+//   P = 2^(s1 - m1) / l1 - lambda 2^(s2 - m2) / l2,   rounded once,
+// with V, once for both maps. Against running both softmaxes beside each other with an
+// output for each, that is the same number of products (scores of 2 x 128 twice, V of 256
+// once, instead of scores once and V twice), half the registers for outputs, no
+// rescaling, and an error of the weights that is relative to the difference.
+//
+// First launch: as prompt attention without its V half; 256 rows of one KV head to a
+// workgroup. Second: rows are (token, head of the group) of a pair of KV heads, 32 of them
+// to two waves; either wave weighs 32 of a tile's 64 tokens for both maps and leaves its
+// weights in LDS, and multiplies all 64 with one of the two V heads: as many products of
+// scores as of V, none done twice. Waves take turns in two groups as in prompt
+// attention, but with two places for tiles: a tile's K, and V of the one before, are sent for
+// at the start of the two phases before those that read it and have arrived at their end.
+// Outputs of 32 bits keep the weights in 2 (f16) or 3 (bf16) 16-bit parts, whose place in LDS
+// leaves room for four waves only.
+#include "prompt_common.h"
+
+#include <algorithm>
+#include <climits>
 
 namespace ema {
 namespace {
 
-__device__ __forceinline__ float to_f32(uint16_t x, int bf16) {
-  return bf16 ? __builtin_bit_cast(float, uint32_t(x) << 16)
-              : float(__builtin_bit_cast(_Float16, x));
+constexpr int kRing = 3;                 // K tiles of the first launch
+constexpr int kStatWaves = 8;
+constexpr int kStatThreads = kStatWaves * 64;
+constexpr int kStatRows = kStatWaves * 32;
+constexpr float kSlack = 8.0f;
+
+// The query head that is head g of KV head kvh's group: heads 2i and 2i + 1 are a pair.
+__device__ __forceinline__ int query_head(int kvh, int group, int g) {
+  return 2 * ((kvh >> 1) * group + g) + (kvh & 1);
 }
 
-__device__ __forceinline__ float wave_max(float x) {
+// Scores of the lane's row that it does not attend become -inf: token 8 * half + t0 + i.
+template <int N>
+__device__ __forceinline__ void mask_scores(f32x16 (&s)[N], int pos, int t0, int half) {
+  const int rel = pos - t0 - half * 8;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-  return x;
-}
-__device__ __forceinline__ float wave_add(float x) {
+  for (int x = 0; x < N; ++x)
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-  return x;
+    for (int i = 0; i < 16; ++i)
+      s[x][i] = x * 32 + (i >> 3) * 16 + (i & 7) <= rel ? s[x][i] : -INFINITY;
 }
 
-// MAPS 1: plain attention of 128 channels; 2: differential attention of 256.
-template <int MAPS>
-__global__ __launch_bounds__(64) void attend_rows(PromptArgs a) {
-  constexpr int D = 128, kCh = 2 * MAPS;               // channels of a lane
-  __shared__ float s_q[MAPS][D], s_p[MAPS][64];
-  const int lane = threadIdx.x, row = blockIdx.x, head = blockIdx.y;
-  int b = row, i = 0, n = 1;
-  if (a.starts) {
-    if (row < a.starts[0] || row >= a.starts[a.batch]) return;
-    int lo = 0, hi = a.batch;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.starts[mid] <= row) lo = mid; else hi = mid;
-    }
-    b = lo;
-    i = row - a.starts[b];
-    n = a.starts[b + 1] - a.starts[b];
-  }
-  const int BS = a.block_size, H = a.kv_heads, G = a.q_heads / H;
-  const int raw = a.seq_lens[b];
-  const int len = max(0, min(raw, a.max_blocks * BS));
-  if (lane == 0 && head == 0 && ((len != raw && i == 0) || (a.starts && len - n + i < 0)))
+template <bool BF16, int BSC>
+__global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int splits) {
+  __shared__ __attribute__((aligned(16))) u32x4 s_k[kRing][kTilePieces];
+  __shared__ int s_find[kFindScratch];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int G = a.q_heads / a.kv_heads;
+  const int kvh = int(blockIdx.x) % a.kv_heads, rest = int(blockIdx.x) / a.kv_heads;
+  const int split = rest % splits;
+  const RowTile R = find_tile<kStatThreads, kStatRows>(a, G, rest / splits, s_find);
+  if (R.b < 0) return;
+  if (R.first == 0 && split == 0 && kvh == 0 && tid == 0 && (R.len < R.n || R.len != R.given))
     atomicAdd(a.err_count, 1);
-  const int seen = a.starts ? len - n + i + 1 : len;   // tokens the row attends
-  const int kvh = head / G * MAPS;                     // the (first) KV head
-  for (int e = lane; e < MAPS * D; e += 64) {
-    const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q) + int64_t(row) * a.q_stride;
-    s_q[e / D][e % D] = to_f32(q[head * MAPS * D + e], a.dtype);
+  const Reach at = reach_of<kStatRows>(R, G, R.first + wave * 32, split, splits);
+  const int j0 = at.j0, j1 = at.j1, head = query_head(kvh, G, at.g);
+
+  u32x4 q[8];
+  {
+    const char* p = a.q + (int64_t(R.row0 + at.tok) * a.q_stride + head * 128 + half * 8) * 2;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
+  }
+  const uint32_t lds_k = lds_address(&s_k[0][0]);
+  constexpr int kTileBytes = kTilePieces * 16;
+  Staging<BSC, kStatThreads> st;
+  // K of tile j + 1 has arrived, K of j + 2 is sent for.
+  auto stage = [&](int j, int s2) {
+    if (j >= j1) return;
+    loads_arrived();
+    if (j + 2 < j1) st.load_k(lds_k + s2 * kTileBytes, j + 2, st.blocks(j + 2), 0);
+  };
+  f32x16 s[2] = {f32x16{}, f32x16{}};
+  const int arow = score_row(col);
+  constexpr int kAhead = 6;
+  auto products = [&](int j, int slot) {
+    if (j >= j1 || j * kKT >= at.wave_end) return;
+    __builtin_amdgcn_s_setprio(1);
+    u32x4 f[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      f[i] = s_k[slot][k_place((i & 1) * 32 + arow, (i >> 1) * 2 + half)];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      s[i & 1] = mfma32<BF16>(f[i], q[i >> 1], i < 2 ? f32x16{} : s[i & 1]);
+    EMA_SCHED_LDS_READ(kAhead);
+#pragma unroll
+    for (int i = 0; i < 16 - kAhead; ++i) {
+      EMA_SCHED_MFMA(1);
+      EMA_SCHED_LDS_READ(1);
+    }
+    EMA_SCHED_MFMA(kAhead);
+    __builtin_amdgcn_s_setprio(0);
+  };
+  float m = -INFINITY, l = 0.0f;
+  auto softmax = [&](int j) {
+    const int t0 = j * kKT;
+    if (t0 >= at.wave_end) return;
+    if (t0 + kKT > at.wave_from + 1) mask_scores(s, at.pos, t0, half);
+    if (st.window.bad != 0) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (st.window.good((t0 + x * 16) >> a.block_shift)) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[x >> 1][(x & 1) * 8 + i] = -INFINITY;
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[tt][i]);
+    mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
+    if (__ballot(mx > m + kSlack)) {
+      const float m_new = fmaxf(m, mx);
+      l *= m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        sum[i & 3] += __builtin_amdgcn_exp2f(fmaf(s[tt][i], a.scale_log2, -ref));
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  };
+  if (j0 < j1) {
+    st.open(a, R.b, kvh, j0, at.end);
+    st.load_k(lds_k, j0, st.blocks(j0), 0);
+    if (j0 + 1 < j1) st.load_k(lds_k + kTileBytes, j0 + 1, st.blocks(j0 + 1), 0);
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) arrived(q[ks]);
+    loads_arrived();
+    __syncthreads();
+    const int late = wave >= kStatWaves / 2 ? 1 : 0;
+    if (late) {
+      stage(j0, 2);
+      __syncthreads();
+    }
+    int s0 = 0, s1 = 1, s2 = 2;          // places of tiles j, j + 1 and j + 2
+    for (int j = j0; j < j1; ++j) {
+      products(j, s0);
+      __syncthreads();
+      stage(j + late, late ? s0 : s2);
+      softmax(j);
+      const int t = s0;
+      s0 = s1;
+      s1 = s2;
+      s2 = t;
+      __syncthreads();
+    }
+    if (!late) __syncthreads();
+    if (st.window.bad != 0 && kvh == 0 && R.first == 0 && tid == 0)
+      atomicAdd(a.err_count, st.window.bad);
+  }
+  l += other_half(l);
+  if (!at.live || half != 0) return;
+  float* ml = a.ws + ((int64_t(split) * a.tokens + R.row0 + at.tok) * a.q_heads + head) * 2;
+  ml[0] = m;
+  ml[1] = l;
+}
+
+template <int NP>
+constexpr int kMulWaves = NP == 1 ? 8 : 4;
+template <int NP>
+constexpr int kMulRows = kMulWaves<NP> / 2 * 32;
+
+template <bool BF16, int BSC, int NP>
+__global__ __launch_bounds__(kMulWaves<NP> * 64, NP == 1 ? 2 : 1)
+void diff_multiply(PromptArgs a, int stat_splits, int splits) {
+  constexpr int kWaves = kMulWaves<NP>, kThreads = kWaves * 64, kRows = kMulRows<NP>;
+  constexpr int kTileBytes = kTilePieces * 16;
+  __shared__ __attribute__((aligned(16))) u32x4 s_k[2][2][kTilePieces];    // [place][KV head]
+  __shared__ __attribute__((aligned(16))) u32x4 s_v[2][2][kTilePieces];
+  __shared__ __attribute__((aligned(16))) u32x4 s_p[kWaves][2][NP][64];    // a wave's weights
+  __shared__ int s_find[kFindScratch];
+  __shared__ int s_bad[2 * 128 + 1];     // the first token not finite, per channel and of all
+  float* const s_sq = reinterpret_cast<float*>(&s_p[0][0][0][0]);          // at the end
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int G = a.q_heads / a.kv_heads, P = a.kv_heads / 2;
+  const int pair = int(blockIdx.x) % P, rest = int(blockIdx.x) / P;
+  const int split = rest % splits;
+  for (int i = tid; i < 2 * 128 + 1; i += kThreads) s_bad[i] = INT_MAX;
+  const RowTile R = find_tile<kThreads, kRows>(a, G, rest / splits, s_find);
+  if (R.b < 0) return;
+  const int mine = wave & 1;             // the half of a tile's tokens, and the V head
+  const Reach at = reach_of<kRows>(R, G, R.first + (wave >> 1) * 32, split, splits);
+  const int j0 = at.j0, j1 = at.j1;
+  const int64_t row = int64_t(R.row0 + at.tok);
+  const int head = pair * G + at.g;      // of the output; its maps are query heads 2h, 2h + 1
+
+  u32x4 q[2][8];
+  float ref[2], by[2];                   // m, and 1 / l (the second map's times lambda)
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const char* p = a.q + (row * a.q_stride + (2 * head + x) * 128 + half * 8) * 2;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) q[x][ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
+    float m = -INFINITY, l = 0.0f;
+    for (int y = 0; y < stat_splits; ++y) {
+      const float* ml = a.ws + ((int64_t(y) * a.tokens + row) * a.q_heads + 2 * head + x) * 2;
+      const float m_new = fmaxf(m, ml[0]), r = m_new == -INFINITY ? 0.0f : m_new;
+      l = l * __builtin_amdgcn_exp2f(m - r) + ml[1] * __builtin_amdgcn_exp2f(ml[0] - r);
+      m = m_new;
+    }
+    ref[x] = m == -INFINITY ? 0.0f : m;
+    by[x] = l == 0.0f ? 0.0f : (x == 0 ? 1.0f : a.lam[head]) / l;
+  }
+
+  const uint32_t lds_k = lds_address(&s_k[0][0][0]), lds_v = lds_address(&s_v[0][0][0]);
+  Staging<BSC, kThreads> st;
+  typename Staging<BSC, kThreads>::Blocks next_v;
+  auto place = [&](int j) { return (j - j0) & 1; };
+  // K of tile j + 1 and V of tile j are sent for.
+  auto send = [&](int j) {
+    if (j >= j1) return;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      st.load_v(lds_v + (place(j) * 2 + x) * kTileBytes, j, next_v, x);
+    if (j + 1 < j1) {
+      next_v = st.blocks(j + 1);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        st.load_k(lds_k + (place(j + 1) * 2 + x) * kTileBytes, j + 1, next_v, x);
+    }
+  };
+  // They are there.
+  auto receive = [&](int j) {
+    if (j >= j1) return;
+    loads_arrived();
+    if ((j + 1) * kKT > at.from + 1 || st.window.bad != 0)
+#pragma unroll 1
+      for (int x = 0; x < 2; ++x)
+        st.template clean_v<BF16>(s_v[place(j)][x], j, at.end, s_bad + x * 128, &s_bad[256]);
+  };
+
+  f32x16 o[4], s[2];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) o[c] = f32x16{};
+  s[0] = s[1] = f32x16{};
+  const int arow = mine * 32 + score_row(col);
+  constexpr int kAhead = NP == 1 ? 6 : 4;
+  auto read_k = [&](int j, int i) {
+    return s_k[place(j)][i & 1][k_place(arow, (i >> 1) * 2 + half)];
+  };
+  auto read_v = [&](int j, int i) {
+    return s_v[place(j)][mine][v_place<BSC>((i & 3) * 32 + col, (i >> 2) * 2 + half)];
+  };
+  // The products of tile j: V of the tile before, K of this one.
+  auto products = [&](int j) {
+    const bool pv = j > j0 && (j - 1) * kKT < at.wave_end, qk = j < j1 && j * kKT < at.wave_end;
+    __builtin_amdgcn_s_setprio(1);
+    u32x4 f[16], g[kAhead];
+    if (pv) {
+      u32x4 w[4][NP];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int n = 0; n < NP; ++n) w[ks][n] = s_p[(wave & ~1) + (ks >> 1)][ks & 1][n][lane];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = read_v(j - 1, i);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) g[i] = read_k(j, i);    // not used where !qk
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int n = 0; n < NP; ++n) o[i & 3] = mfma32<BF16>(f[i], w[i >> 2][n], o[i & 3]);
+      EMA_SCHED_LDS_READ(4 * NP + kAhead);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        EMA_SCHED_MFMA(NP);
+        EMA_SCHED_LDS_READ(1);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) g[i] = read_k(j, i);
+    }
+    if (qk) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = i < kAhead ? g[i] : read_k(j, i);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        s[i & 1] = mfma32<BF16>(f[i], q[i & 1][i >> 1], i < 2 ? f32x16{} : s[i & 1]);
+#pragma unroll
+      for (int i = 0; i < 16 - kAhead; ++i) {
+        EMA_SCHED_MFMA(1);
+        EMA_SCHED_LDS_READ(1);
+      }
+      EMA_SCHED_MFMA(kAhead);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+  // The weights of this wave's 32 tokens of tile j.
+  auto weigh = [&](int j) {
+    const int t0 = j * kKT + mine * 32;
+    if (j * kKT >= at.wave_end) return;
+    if (t0 + 32 > at.wave_from + 1) {
+      const int rel = at.pos - t0 - half * 8;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          s[x][i] = (i >> 3) * 16 + (i & 7) <= rel ? s[x][i] : -INFINITY;
+    }
+    if (st.window.bad != 0) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        if (st.window.good((t0 + y * 16) >> a.block_shift)) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[0][y * 8 + i] = s[1][y * 8 + i] = -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4 w[NP];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        float p[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int i = ks * 8 + 2 * y + e;
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[0][i], a.scale_log2, -ref[0]));
+          const float p2 = __builtin_amdgcn_exp2f(fmaf(s[1][i], a.scale_log2, -ref[1]));
+          p[e] = fmaf(p1, by[0], -(p2 * by[1]));
+        }
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+          const uint32_t u = pack16<BF16>(p[0], p[1]);
+          w[n][y] = u;
+          p[0] -= low16<BF16>(u);
+          p[1] -= high16<BF16>(u);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NP; ++n) s_p[wave][ks][n][lane] = w[n];
+    }
+  };
+
+  if (j0 < j1) {
+    st.open(a, R.b, 2 * pair, j0, at.end);
+    next_v = st.blocks(j0);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) st.load_k(lds_k + x * kTileBytes, j0, next_v, x);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) arrived(q[x][ks]);
+      arrived(ref[x]);
+      arrived(by[x]);
+    }
+    loads_arrived();
+    __syncthreads();
+    // Phase 2j: the first group has the products of tile j, the second weighs tile j - 1;
+    // 2j + 1: the other way round. Both send at the start of 2j and receive at the end of
+    // 2j + 1.
+    const int late = NP == 1 && wave >= kWaves / 2 ? 1 : 0;
+    if (late) {
+      send(j0);
+      __syncthreads();
+    }
+    for (int j = j0; j < j1; ++j) {
+      if (!late) send(j);
+      products(j);
+      if (late) receive(j);
+      __syncthreads();
+      if (late) send(j + 1);
+      weigh(j);
+      if (!late) receive(j);
+      __syncthreads();
+    }
+    products(j1);
+    if (!late) __syncthreads();
   }
   __syncthreads();
-  float m[MAPS], l[MAPS], o[MAPS][kCh];
+
+  if (s_bad[256] != INT_MAX)
 #pragma unroll
-  for (int x = 0; x < MAPS; ++x) {
-    m[x] = -INFINITY;
-    l[x] = 0.0f;
+    for (int c = 0; c < 4; ++c)
 #pragma unroll
-    for (int c = 0; c < kCh; ++c) o[x][c] = 0.0f;
+      for (int i = 0; i < 16; ++i)
+        if (at.pos >= s_bad[mine * 128 + c * 32 + (i >> 2) * 8 + half * 4 + (i & 3)]) o[c][i] = NAN;
+  if (splits > 1) {
+    if (!at.live) return;
+    float* po = a.ws + int64_t(stat_splits) * a.tokens * a.q_heads * 2 +
+                ((int64_t(split) * a.tokens + row) * (a.q_heads / 2) + head) * 256 + mine * 128;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(po + c * 32 + i * 8 + half * 4) =
+            f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
+    return;
   }
-  const int64_t half = int64_t(BS) * H * D;
-  for (int t0 = 0; t0 < seen; t0 += 64) {
-    const int t = t0 + lane;
-    int id = -1;
-    if (t < seen) {
-      id = a.table[int64_t(b) * a.max_blocks + t / BS];
-      if (id < 0 || id >= a.n_local) {
-        if (t % BS == 0 && head == 0) atomicAdd(a.err_count, 1);
-        id = -1;
-      }
-    }
-    const uint16_t* blk = reinterpret_cast<const uint16_t*>(a.local + int64_t(max(id, 0)) * a.block_bytes);
+  float inv = 1.0f;
+  if (a.norm_weight) {
+    float sq = 0.0f;
 #pragma unroll
-    for (int x = 0; x < MAPS; ++x) {
-      float s = -INFINITY;
-      if (id >= 0) {
-        s = 0.0f;
-        const uint16_t* k = blk + (int64_t(kvh + x) * BS + t % BS) * D;
-        for (int d = 0; d < D; ++d) s = fmaf(to_f32(k[d], a.dtype), s_q[x][d], s);
-        s *= a.scale_log2;
-      }
-      const float mx = fmaxf(m[x], wave_max(s));
-      const float at = mx == -INFINITY ? 0.0f : mx;      // NaN scores stay NaN
-      const float f = exp2f(m[x] - at);
-      const float p = exp2f(s - at);
-      m[x] = mx;
-      l[x] = l[x] * f + wave_add(p);
+    for (int c = 0; c < 4; ++c)
 #pragma unroll
-      for (int c = 0; c < kCh; ++c) o[x][c] *= f;
-      s_p[x][lane] = p;
-    }
+      for (int i = 0; i < 16; ++i) sq = fmaf(o[c][i], o[c][i], sq);
+    sq += other_half(sq);
+    s_sq[wave * 64 + lane] = sq;
     __syncthreads();
-    for (int k = 0; k < 64; ++k) {
-      const int kid = __shfl(id, k);
-      if (kid < 0) continue;
-      const uint16_t* kb = reinterpret_cast<const uint16_t*>(a.local + int64_t(kid) * a.block_bytes) + half;
+    sq += s_sq[(wave ^ 1) * 64 + lane];
+    inv = sq == 0.0f ? 0.0f : 1.0f / sqrtf(sq / 256.0f + a.norm_eps);
+  }
+  if (!at.live) return;
+  AttnArgs to;
+  to.out = a.out;
+  to.out_dtype = a.out_dtype;
+  to.out_vec = 1;
 #pragma unroll
-      for (int c = 0; c < kCh; ++c) {
-        const float v = to_f32(kb[(int64_t(kvh) * D + c * 64 + lane) * BS + (t0 + k) % BS], a.dtype);
+  for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int x = 0; x < MAPS; ++x) o[x][c] = fmaf(s_p[x][k], v, o[x][c]);
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int d = mine * 128 + c * 32 + i * 8 + half * 4;
+      f32x4 r = f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]} * inv;
+      if (a.norm_weight) r *= *reinterpret_cast<const f32x4*>(a.norm_weight + d);
+      store_out4(to, (row * (a.q_heads / 2) + head) * 256 + d, out_f32x4{r[0], r[1], r[2], r[3]});
     }
-    __syncthreads();
-  }
-  AttnArgs st;
-  st.out = a.out;
-  st.out_dtype = a.out_dtype;
-  float r[kCh], sq = 0.0f;
-#pragma unroll
-  for (int c = 0; c < kCh; ++c) {
-    r[c] = l[0] == 0.0f ? 0.0f : o[0][c] / l[0];
-    if constexpr (MAPS == 2) r[c] -= l[1] == 0.0f ? 0.0f : a.lam[head] * (o[1][c] / l[1]);
-    sq = fmaf(r[c], r[c], sq);
-  }
-  if (MAPS == 2 && a.norm_weight) {
-    const float inv = 1.0f / sqrtf(wave_add(sq) / float(MAPS * D) + a.norm_eps);
-#pragma unroll
-    for (int c = 0; c < kCh; ++c) r[c] *= inv * a.norm_weight[c * 64 + lane];
-  }
-#pragma unroll
-  for (int c = 0; c < kCh; ++c)
-    store_out(st, (int64_t(row) * (a.q_heads / MAPS) + head) * MAPS * D + c * 64 + lane, r[c]);
 }
 
-template <int MAPS>
-hipError_t launch(const PromptArgs& a, hipStream_t stream) {
-  if (a.tokens <= 0 || a.batch <= 0) return hipSuccess;
-  hipLaunchKernelGGL(attend_rows<MAPS>, dim3(a.tokens, a.q_heads / MAPS), dim3(64), 0, stream, a);
+// Adds up the parts of a row: a wave to a row, four channels a lane.
+__global__ __launch_bounds__(256) void diff_add(PromptArgs a, int stat_splits, int splits) {
+  const int64_t rows = int64_t(a.tokens) * (a.q_heads / 2);
+  const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  const int tok = int(row / (a.q_heads / 2));
+  if (tok < a.starts[0] || tok >= a.starts[a.batch]) return;
+  const int lane = threadIdx.x & 63;
+  const float* parts = a.ws + int64_t(stat_splits) * a.tokens * a.q_heads * 2;
+  f32x4 r = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s)
+    r += *reinterpret_cast<const f32x4*>(parts + (s * rows + row) * 256 + 4 * lane);
+  if (a.norm_weight) {
+    float sq = r[0] * r[0] + r[1] * r[1] + r[2] * r[2] + r[3] * r[3];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sq += __shfl_xor(sq, o);
+    const float inv = sq == 0.0f ? 0.0f : 1.0f / sqrtf(sq / 256.0f + a.norm_eps);
+    r *= *reinterpret_cast<const f32x4*>(a.norm_weight + 4 * lane) * inv;
+  }
+  AttnArgs to;
+  to.out = a.out;
+  to.out_dtype = a.out_dtype;
+  to.out_vec = 1;
+  store_out4(to, row * 256 + 4 * lane, out_f32x4{r[0], r[1], r[2], r[3]});
+}
+
+// How the two launches are cut: tiles of rows at most, whatever the lengths, and the parts
+// that a tile's tokens are cut into (as many as fill 256 compute units, of 256 tokens at
+// least where the table is full).
+struct Cut {
+  int64_t stat_tiles, mul_tiles;
+  int stat_splits, mul_splits;
+};
+Cut cut_of(const PromptArgs& a) {
+  const int64_t rows = int64_t(a.tokens) * (a.q_heads / a.kv_heads);
+  const int64_t most = int64_t(a.max_blocks) * a.block_size / 256;
+  const int mul_rows = a.out_dtype == kOutF32 ? kMulRows<2> : kMulRows<1>;
+  auto tiles = [&](int n) {
+    return std::min<int64_t>(a.tokens, (rows + n - 1) / n + a.batch - 1);
+  };
+  auto splits = [&](int64_t groups) {
+    return int(std::max<int64_t>(1, std::min<int64_t>({256 / groups, most, 64})));
+  };
+  Cut c;
+  c.stat_tiles = tiles(kStatRows);
+  c.mul_tiles = tiles(mul_rows);
+  c.stat_splits = splits(c.stat_tiles * a.kv_heads);
+  c.mul_splits = splits(c.mul_tiles * (a.kv_heads / 2));
+  return c;
+}
+
+template <bool BF16, int BSC, int NP>
+hipError_t launch(const PromptArgs& a, const Cut& c, hipStream_t stream) {
+  hipLaunchKernelGGL((diff_stats<BF16, BSC>),
+                     dim3(unsigned(c.stat_tiles * a.kv_heads * c.stat_splits)), dim3(kStatThreads),
+                     0, stream, a, c.stat_splits);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((diff_multiply<BF16, BSC, NP>),
+                     dim3(unsigned(c.mul_tiles * (a.kv_heads / 2) * c.mul_splits)),
+                     dim3(kMulWaves<NP> * 64), 0, stream, a, c.stat_splits, c.mul_splits);
   return hipGetLastError();
+}
+
+template <bool BF16, int NP>
+hipError_t launch_sizes(const PromptArgs& a, const Cut& c, hipStream_t stream) {
+  return a.block_size == 16   ? launch<BF16, 16, NP>(a, c, stream)
+         : a.block_size == 32 ? launch<BF16, 32, NP>(a, c, stream)
+                              : launch<BF16, 64, NP>(a, c, stream);
 }
 
 }  // namespace
 
-size_t diff_prompt_workspace(const PromptArgs&) { return 0; }
-hipError_t launch_diff_prompt_attention(const PromptArgs& a, hipStream_t s) { return launch<2>(a, s); }
+size_t diff_prompt_workspace(const PromptArgs& a) {
+  // the output's type is not known here: the larger of the two cuts
+  PromptArgs b = a;
+  size_t most = 0;
+  for (int out : {kOutF32, kOutBF16}) {
+    b.out_dtype = out;
+    const Cut c = cut_of(b);
+    size_t n = size_t(c.stat_splits) * a.tokens * a.q_heads * 2;
+    if (c.mul_splits > 1) n += size_t(c.mul_splits) * a.tokens * (a.q_heads / 2) * 256;
+    most = std::max(most, n);
+  }
+  return most * 4;
+}
+
+hipError_t launch_diff_prompt_attention(const PromptArgs& a, hipStream_t stream) {
+  const Cut c = cut_of(a);
+  hipError_t e;
+  if (a.out_dtype != kOutF32)
+    e = a.dtype == 1 ? launch_sizes<true, 1>(a, c, stream) : launch_sizes<false, 1>(a, c, stream);
+  else
+    e = a.dtype == 1 ? launch_sizes<true, 3>(a, c, stream) : launch_sizes<false, 2>(a, c, stream);
+  if (e != hipSuccess || c.mul_splits == 1) return e;
+  const int64_t rows = int64_t(a.tokens) * (a.q_heads / 2);
+  hipLaunchKernelGGL(diff_add, dim3(unsigned((rows + 3) / 4)), dim3(256), 0, stream, a,
+                     c.stat_splits, c.mul_splits);
+  return hipGetLastError();
+}
 
 }  // namespace ema

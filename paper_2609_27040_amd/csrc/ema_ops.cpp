@@ -241,8 +241,8 @@ int attention(const AttnCall& c) {
       return inval(c.what, "NULL array");
     if (c.q_stride < int64_t(c.num_q_heads) * h->shape.head_dim || c.q_stride % 8 != 0)
       return inval(c.what, "q_stride must be a multiple of 8 that holds a token's heads");
-    if (!h->host_only && (!aligned16(c.q) || !aligned16(c.out)))
-      return inval(c.what, "q and out must be 16-byte aligned");
+    if (!h->host_only && (!aligned16(c.q) || !aligned16(c.out) || !aligned16(c.norm_weight)))
+      return inval(c.what, "q, out and norm_weight must be 16-byte aligned");
   }
   if (c.tokens == 0 || c.batch == 0) return EMA_OK;
   if (!h->host_only && h->book.n_local() == 0) return inval(c.what, "the local pool is empty");

@@ -22,7 +22,6 @@ namespace ema {
 namespace {
 
 constexpr int kWaves = 8;
-constexpr int kPieces = kTilePieces / (kWaves * 64);   // of K, and of V, to a thread
 constexpr int kThreads = kWaves * 64;
 constexpr int kRows = kWaves * 32;
 constexpr int kRing = 3;                 // staged tiles
@@ -71,108 +70,34 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
   if (tid < 129) s_bad[tid] = INT_MAX;
   const RowTile R = find_tile<kThreads, kRows>(a, G, rest / splits, s_find);
   if (R.b < 0) return;
-  const int past = R.len - R.n;          // tokens before the chunk
-  if (R.first == 0 && split == 0 && kvh == 0 && tid == 0 &&
-      (past < 0 || R.len != R.given))
+  if (R.first == 0 && split == 0 && kvh == 0 && tid == 0 && (R.len < R.n || R.len != R.given))
     atomicAdd(a.err_count, 1);
-
-  const int r = R.first + wave * 32 + col;
-  const bool live = r < R.n * G;
-  const int tok = live ? r / G : 0, g = live ? r - tok * G : 0;
-  const int pos = live ? past + tok : -1;              // the row attends tokens 0 .. pos
-  const int last_row = min(R.n * G, R.first + kRows) - 1;
-  const int end = uniform(max(0, past + last_row / G + 1));   // tokens the workgroup looks at
-  const int from = uniform(past + R.first / G);        // position of its first row
-  const int wave_first = R.first + wave * 32;
-  const int wave_end = uniform(wave_first >= R.n * G
-                                   ? 0 : max(0, past + min(R.n * G - 1, wave_first + 31) / G + 1));
-  const int wave_from = uniform(past + wave_first / G);
-  const int n_tiles = (end + kKT - 1) / kKT;
-  const int j0 = uniform(int(int64_t(n_tiles) * split / splits));
-  const int j1 = uniform(int(int64_t(n_tiles) * (split + 1) / splits));
+  const Reach at = reach_of<kRows>(R, G, R.first + wave * 32, split, splits);
+  const int j0 = at.j0, j1 = at.j1;
 
   u32x4 q[8];
   {
-    const char* p = a.q + (int64_t(R.row0 + tok) * a.q_stride + (kvh * G + g) * 128 + half * 8) * 2;
+    const char* p = a.q + (int64_t(R.row0 + at.tok) * a.q_stride + (kvh * G + at.g) * 128 + half * 8) * 2;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
   }
 
   // ---- staging -------------------------------------------------------------------
-  // Place p of a tile's K and of its V in LDS is loaded by thread p % kThreads; which piece
-  // belongs there is in the offsets. A wave's 64 places of one round lie in one block, the
-  // same for K and V.
-  const int64_t v_half = a.block_bytes / 2;
-  const int last_block = (max(end, 1) - 1) >> a.block_shift;
-  constexpr int kPer = 16 * BSC;                               // pieces of a block
-  uint32_t k_off[kPieces], v_off[kPieces];                     // bytes in the block
-  int v_ch[kPieces], v_tok[kPieces];                           // the V piece's channel and first token
-#pragma unroll
-  for (int x = 0; x < kPieces; ++x) {
-    const int p = x * kThreads + tid;
-    const int kt = p >> 4;
-    k_off[x] = ((kvh * a.block_size + kt % BSC) * 128 + ((p ^ kt) & 15) * 8) * 2;
-    const int vb = p / kPer, ch = p % kPer / (BSC / 8), gi = p % (BSC / 8) ^ v_turn<BSC>(ch);
-    v_off[x] = v_half + ((kvh * 128 + ch) * a.block_size + gi * 8) * 2;
-    v_ch[x] = ch;
-    v_tok[x] = vb * BSC + gi * 8;
-  }
-  const uint32_t lds_k = lds_address(&s_k[0][0]) + wave * 1024;
-  const uint32_t lds_v = lds_address(&s_v[0][0]) + wave * 1024;
-  IdWindow window;
-  struct Blocks {
-    const char* at[kPieces];             // the blocks of this wave's places
-  };
-  auto blocks_of = [&](int j) {
-    Blocks t;
-    const int first = j * kKT >> a.block_shift;
-    window.seek(min(first, last_block));
-    const int tb = BSC == 64 ? (j * kKT) & (a.block_size - 1) : 0;
-#pragma unroll
-    for (int x = 0; x < kPieces; ++x)
-      t.at[x] = a.local + int64_t(window.get(min(first + (x * kThreads + wave * 64) / kPer,
-                                                 last_block))) * a.block_bytes + tb * 2;
-    return t;
-  };
-  auto load_k = [&](int slot, int j, const Blocks& t) {
-    const int tb = BSC == 64 ? (j * kKT) & (a.block_size - 1) : 0;
-#pragma unroll
-    for (int x = 0; x < kPieces; ++x)
-      load_to_lds(t.at[x] + tb * 254, k_off[x],
-                  lds_k + slot * (kTilePieces * 16) + x * kThreads * 16);
-  };
-  auto load_v = [&](int slot, const Blocks& t) {
-#pragma unroll
-    for (int x = 0; x < kPieces; ++x)
-      load_to_lds(t.at[x], v_off[x], lds_v + slot * (kTilePieces * 16) + x * kThreads * 16);
-  };
-  // V of tokens that are not there becomes 0, in the pieces this thread loaded.
-  auto clean_v = [&](int slot, int j) {
-    if ((j + 1) * kKT <= from + 1 && window.bad == 0) return;  // no row masks any token
-#pragma unroll
-    for (int x = 0; x < kPieces; ++x) {
-      u32x4* at = &s_v[slot][x * kThreads + tid];
-      u32x4 v = *at;
-      const int tok = j * kKT + v_tok[x];
-      const int left = window.bad == 0 || window.good(tok >> a.block_shift) ? end - tok : 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        v[i] &= (2 * i < left ? 0xffffu : 0u) | (2 * i + 1 < left ? 0xffff0000u : 0u);
-      if (not_finite<BF16>(v)) drop_not_finite<BF16>(v, tok, &s_bad[v_ch[x]], &s_bad[128]);
-      *at = v;
-    }
-  };
-  Blocks next_v;                         // of the K tile on its way, whose V is next
+  const uint32_t lds_k = lds_address(&s_k[0][0]), lds_v = lds_address(&s_v[0][0]);
+  constexpr int kTileBytes = kTilePieces * 16;
+  Staging<BSC, kThreads> st;
+  typename Staging<BSC, kThreads>::Blocks next_v;   // of the K tile on its way, whose V is next
   // Step j: V of tile j and K of tile j + 1 have arrived; V of j + 1 and K of j + 2 are
   // sent for. s0, s1, s2: places of tiles j, j + 1 and j + 2.
   auto stage = [&](int j, int s0, int s1, int s2) {
     if (j >= j1) return;
     loads_arrived();
-    clean_v(s0, j);
-    if (j + 1 < j1) load_v(s1, next_v);
+    if ((j + 1) * kKT > at.from + 1 || st.window.bad != 0)      // some row masks some token
+      st.template clean_v<BF16>(s_v[s0], j, at.end, s_bad, &s_bad[128]);
+    if (j + 1 < j1) st.load_v(lds_v + s1 * kTileBytes, j + 1, next_v, 0);
     if (j + 2 < j1) {
-      next_v = blocks_of(j + 2);
-      load_k(s2, j + 2, next_v);
+      next_v = st.blocks(j + 2);
+      st.load_k(lds_k + s2 * kTileBytes, j + 2, next_v, 0);
     }
   };
 
@@ -182,8 +107,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
   for (int c = 0; c < 4; ++c) o[c] = f32x16{};
   s[0] = s[1] = f32x16{};
   Weights<NP> w;
-  // A rows of the scores: MFMA row i of a 32-token tile is this token
-  const int arow = (col >> 4) * 16 + ((col >> 2) & 1) * 8 + ((col >> 3) & 1) * 4 + (col & 3);
+  const int arow = score_row(col);
   // operands this many products ahead of their use (fewer where registers are short)
   constexpr int kAhead = NP == 3 ? 4 : 6;
   auto read_k = [&](int slot, int i) {
@@ -201,7 +125,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
   };
   // The products of tile j: V of the tile before, K of this one, from their places.
   auto products = [&](int j, int before, int slot) {
-    const bool pv = j > j0 && (j - 1) * kKT < wave_end, qk = j < j1 && j * kKT < wave_end;
+    const bool pv = j > j0 && (j - 1) * kKT < at.wave_end, qk = j < j1 && j * kKT < at.wave_end;
     __builtin_amdgcn_s_setprio(1);
     u32x4 f[16], g[kAhead];
     if (pv) {
@@ -240,19 +164,19 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
   float m = -INFINITY, l = 0.0f;         // l: this lane's half of the tokens
   auto softmax = [&](int j) {
     const int t0 = j * kKT;
-    if (j >= j1 || t0 >= wave_end) return;
-    if (t0 + kKT > wave_from + 1) {
-      const int rel = pos - t0 - half * 8;             // token 16k + e of this lane: 16k + e <= rel
+    if (j >= j1 || t0 >= at.wave_end) return;
+    if (t0 + kKT > at.wave_from + 1) {
+      const int rel = at.pos - t0 - half * 8;             // token 16k + e of this lane: 16k + e <= rel
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           s[tt][i] = tt * 32 + (i >> 3) * 16 + (i & 7) <= rel ? s[tt][i] : -INFINITY;
     }
-    if (window.bad != 0) {
+    if (st.window.bad != 0) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) {                    // 16 tokens, in one block
-        if (window.good((t0 + x * 16) >> a.block_shift)) continue;
+        if (st.window.good((t0 + x * 16) >> a.block_shift)) continue;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[x >> 1][(x & 1) * 8 + i] = -INFINITY;
       }
@@ -289,13 +213,13 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
 
   // ---- the phases ----------------------------------------------------------------
   if (j0 < j1) {
-    window.open(a, R.b, j0 * kKT >> a.block_shift, last_block);
-    next_v = blocks_of(j0);
-    load_k(0, j0, next_v);
-    load_v(0, next_v);
+    st.open(a, R.b, kvh, j0, at.end);
+    next_v = st.blocks(j0);
+    st.load_k(lds_k, j0, next_v, 0);
+    st.load_v(lds_v, j0, next_v, 0);
     if (j0 + 1 < j1) {
-      next_v = blocks_of(j0 + 1);
-      load_k(1, j0 + 1, next_v);
+      next_v = st.blocks(j0 + 1);
+      st.load_k(lds_k + kTileBytes, j0 + 1, next_v, 0);
     }
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) arrived(q[ks]);
@@ -321,19 +245,20 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
     }
     products(j1, s2, s0);
     if (!late) __syncthreads();
-    if (window.bad != 0 && kvh == 0 && R.first == 0 && tid == 0) atomicAdd(a.err_count, window.bad);
+    if (st.window.bad != 0 && kvh == 0 && R.first == 0 && tid == 0)
+      atomicAdd(a.err_count, st.window.bad);
   }
   __syncthreads();
 
   l += other_half(l);
-  if (!live) return;
+  if (!at.live) return;
   if (s_bad[128] != INT_MAX)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (pos >= s_bad[c * 32 + (i >> 2) * 8 + half * 4 + (i & 3)]) o[c][i] = NAN;
-  const int64_t orow = int64_t(R.row0 + tok) * a.q_heads + kvh * G + g;
+        if (at.pos >= s_bad[c * 32 + (i >> 2) * 8 + half * 4 + (i & 3)]) o[c][i] = NAN;
+  const int64_t orow = int64_t(R.row0 + at.tok) * a.q_heads + kvh * G + at.g;
   if (splits > 1) {
     const int64_t part = int64_t(split) * a.tokens * a.q_heads + orow;
     float* po = a.ws + part * 128;
@@ -350,16 +275,16 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
     }
     return;
   }
-  AttnArgs st;
-  st.out = a.out;
-  st.out_dtype = a.out_dtype;
-  st.out_vec = 1;
+  AttnArgs to;
+  to.out = a.out;
+  to.out_dtype = a.out_dtype;
+  to.out_vec = 1;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      store_out4(st, orow * 128 + c * 32 + i * 8 + half * 4,
+      store_out4(to, orow * 128 + c * 32 + i * 8 + half * 4,
                  out_f32x4{o[c][4 * i] * inv, o[c][4 * i + 1] * inv, o[c][4 * i + 2] * inv,
                            o[c][4 * i + 3] * inv});
 }

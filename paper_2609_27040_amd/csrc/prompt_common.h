@@ -28,6 +28,12 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+// MFMA row i of a 32-token tile of scores is this token of it: every lane then has 8
+// consecutive tokens, 8 * (lane / 32) on, of both 16-token halves.
+__device__ __forceinline__ int score_row(int i) {
+  return (i >> 4) * 16 + ((i >> 2) & 1) * 8 + ((i >> 3) & 1) * 4 + (i & 3);
+}
+
 // Two floats rounded to nearest into 16-bit halves of a word, and back.
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack16(float x, float y) {
@@ -260,6 +266,36 @@ __device__ __forceinline__ RowTile find_tile(const PromptArgs& a, int group, int
 }
 constexpr int kFindScratch = 16 + 4;
 
+// The row of a lane and the tokens that it, its wave's 32 rows and its workgroup look at.
+struct Reach {
+  bool live;              // there is such a row
+  int tok, g;             // its token of the chunk, its head of the group
+  int pos;                // it attends tokens 0 .. pos
+  int end, from;          // workgroup: tokens looked at; position of its first row
+  int wave_end, wave_from;
+  int j0, j1;             // tiles of this split
+};
+// `first`: the wave's first row, counted from the sequence's.
+template <int ROWS>
+__device__ __forceinline__ Reach reach_of(const RowTile& R, int group, int first, int split,
+                                          int splits) {
+  Reach x;
+  const int past = R.len - R.n, rows = R.n * group;  // tokens before the chunk
+  const int r = first + (threadIdx.x & 31);
+  x.live = r < rows;
+  x.tok = x.live ? r / group : 0;
+  x.g = x.live ? r - x.tok * group : 0;
+  x.pos = x.live ? past + x.tok : -1;
+  x.end = uniform(max(0, past + (min(rows, R.first + ROWS) - 1) / group + 1));
+  x.from = uniform(past + R.first / group);
+  x.wave_end = uniform(first >= rows ? 0 : max(0, past + min(rows - 1, first + 31) / group + 1));
+  x.wave_from = uniform(past + first / group);
+  const int tiles = (x.end + 63) / 64;
+  x.j0 = uniform(int(int64_t(tiles) * split / splits));
+  x.j1 = uniform(int(int64_t(tiles) * (split + 1) / splits));
+  return x;
+}
+
 // ---- staged tiles --------------------------------------------------------------------
 //
 // K: row t (256 bytes, 16 pieces) as it is, its pieces permuted by t so that the 16
@@ -353,6 +389,96 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return uint32_t(reinterpret_cast<uintptr_t>(
       (const __attribute__((address_space(3))) void*)p));
 }
+
+// Loads tiles of K and V of a workgroup's sequence into LDS. Place p of a tile is loaded by
+// thread p % THREADS; which piece belongs there is in the offsets. A wave's 64 places of one
+// round lie in one block, the same for K and V. `head` counts from the workgroup's first KV
+// head: a head's K and V both take 256 * block_size bytes.
+template <int BSC, int THREADS>
+struct Staging {
+  static constexpr int kPieces = kTilePieces / THREADS;
+  static constexpr int kPer = 16 * BSC;              // pieces of a block
+  struct Blocks {
+    const char* at[kPieces];                         // the blocks of this wave's places
+  };
+  const char* local;
+  int64_t block_bytes;
+  int shift, mask, last, head_bytes, wave;
+  uint32_t k_off[kPieces], v_off[kPieces];           // bytes in the block
+  IdWindow window;
+
+  // Of sequence b, whose first `end` tokens (one at least) are looked at, from tile j0 on.
+  __device__ __forceinline__ void open(const PromptArgs& a, int b, int kvh, int j0, int end) {
+    const int tid = threadIdx.x;
+    local = a.local;
+    block_bytes = a.block_bytes;
+    shift = a.block_shift;
+    mask = a.block_size - 1;
+    head_bytes = 256 * a.block_size;
+    wave = uniform(tid >> 6);
+    last = (end - 1) >> shift;
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      const int p = x * THREADS + tid, kt = p >> 4;
+      k_off[x] = kvh * head_bytes + (kt % BSC * 128 + ((p ^ kt) & 15) * 8) * 2;
+      v_off[x] = uint32_t(a.block_bytes / 2) + kvh * head_bytes +
+                 (channel(x) * a.block_size + group(x) * 8) * 2;
+    }
+    window.open(a, b, (j0 * kKT) >> shift, last);
+  }
+  // The channel, the eight tokens of its block and the first token of the tile that piece x of
+  // this thread's V is.
+  static __device__ __forceinline__ int channel(int x) {
+    return (x * THREADS + int(threadIdx.x)) % kPer / (BSC / 8);
+  }
+  static __device__ __forceinline__ int group(int x) {
+    return (x * THREADS + int(threadIdx.x)) % (BSC / 8) ^ v_turn<BSC>(channel(x));
+  }
+  static __device__ __forceinline__ int token(int x) {
+    return (x * THREADS + int(threadIdx.x)) / kPer * BSC + group(x) * 8;
+  }
+  // Where tile j's pieces are; tiles in ascending order.
+  __device__ __forceinline__ Blocks blocks(int j) {
+    Blocks t;
+    const int first = (j * kKT) >> shift;
+    window.seek(min(first, last));
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x)
+      t.at[x] = local + int64_t(window.get(min(first + (x * THREADS + wave * 64) / kPer, last))) *
+                            block_bytes;
+    return t;
+  }
+  // `to`: the tile's address in LDS.
+  __device__ __forceinline__ void load_k(uint32_t to, int j, const Blocks& t, int head) const {
+    const int in = BSC == 64 ? ((j * kKT) & mask) * 256 : 0;   // of block size 128 and more
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x)
+      load_to_lds(t.at[x] + in + head * head_bytes, k_off[x], to + (x * THREADS + wave * 64) * 16);
+  }
+  __device__ __forceinline__ void load_v(uint32_t to, int j, const Blocks& t, int head) const {
+    const int in = BSC == 64 ? ((j * kKT) & mask) * 2 : 0;
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x)
+      load_to_lds(t.at[x] + in + head * head_bytes, v_off[x], to + (x * THREADS + wave * 64) * 16);
+  }
+  // In the pieces this thread has loaded of V tile j: V of tokens from `end` on or in no block
+  // of the pool becomes 0, and so does what is not finite (noted in first[channel], any).
+  template <bool BF16>
+  __device__ __forceinline__ void clean_v(u32x4* tile, int j, int end, int* first, int* any) const {
+#pragma unroll
+    for (int x = 0; x < kPieces; ++x) {
+      u32x4* at = tile + x * THREADS + threadIdx.x;
+      u32x4 v = *at;
+      const int tok = j * kKT + token(x);
+      const int left = window.bad == 0 || window.good(tok >> shift) ? end - tok : 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[i] &= (2 * i < left ? 0xffffu : 0u) | (2 * i + 1 < left ? 0xffff0000u : 0u);
+      if (not_finite<BF16>(v)) drop_not_finite<BF16>(v, tok, first + channel(x), any);
+      *at = v;
+    }
+  }
+};
 
 // Order of what the scheduler lays out next, `n` instructions at a time.
 #define EMA_SCHED_VALU(n) __builtin_amdgcn_sched_group_barrier(0x2, n, 0)
