@@ -209,11 +209,22 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) q[x][ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
     float m = -INFINITY, l = 0.0f;
-    for (int y = 0; y < stat_splits; ++y) {
-      const float* ml = a.ws + ((int64_t(y) * a.tokens + row) * a.q_heads + 2 * head + x) * 2;
-      const float m_new = fmaxf(m, ml[0]), r = m_new == -INFINITY ? 0.0f : m_new;
-      l = l * __builtin_amdgcn_exp2f(m - r) + ml[1] * __builtin_amdgcn_exp2f(ml[0] - r);
-      m = m_new;
+    const int64_t step = int64_t(a.tokens) * a.q_heads * 2;
+    const float* ml = a.ws + (row * a.q_heads + 2 * head + x) * 2;
+    for (int y0 = 0; y0 < stat_splits; y0 += 8) {      // eight parts in a round trip
+      float pm[8], pl[8];
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        pm[y] = ml[min(y0 + y, stat_splits - 1) * step];
+        pl[y] = ml[min(y0 + y, stat_splits - 1) * step + 1];
+      }
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        if (y0 + y >= stat_splits) break;
+        const float m_new = fmaxf(m, pm[y]), r = m_new == -INFINITY ? 0.0f : m_new;
+        l = l * __builtin_amdgcn_exp2f(m - r) + pl[y] * __builtin_amdgcn_exp2f(pm[y] - r);
+        m = m_new;
+      }
     }
     ref[x] = m == -INFINITY ? 0.0f : m;
     by[x] = l == 0.0f ? 0.0f : (x == 0 ? 1.0f : a.lam[head]) / l;
@@ -391,16 +402,12 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (at.pos >= s_bad[mine * 128 + c * 32 + (i >> 2) * 8 + half * 4 + (i & 3)]) o[c][i] = NAN;
+  u32x4* const scratch = &s_k[0][0][0] + wave * 512;
+  const int out_row = at.live ? int(row) * (a.q_heads / 2) + head : -1;
   if (splits > 1) {
-    if (!at.live) return;
-    float* po = a.ws + int64_t(stat_splits) * a.tokens * a.q_heads * 2 +
-                ((int64_t(split) * a.tokens + row) * (a.q_heads / 2) + head) * 256 + mine * 128;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(po + c * 32 + i * 8 + half * 4) =
-            f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
+    const int64_t rows = int64_t(a.tokens) * (a.q_heads / 2);
+    write_rows(scratch, o, 1.0f, out_row, 256, mine * 128,
+               a.ws + int64_t(stat_splits) * a.tokens * a.q_heads * 2 + split * rows * 256, kOutF32);
     return;
   }
   float inv = 1.0f;
@@ -415,21 +422,17 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
     __syncthreads();
     sq += s_sq[(wave ^ 1) * 64 + lane];
     inv = sq == 0.0f ? 0.0f : 1.0f / sqrtf(sq / 256.0f + a.norm_eps);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(a.norm_weight + mine * 128 + c * 32 + i * 8 +
+                                                        half * 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[c][4 * i + k] *= x[k];
+      }
   }
-  if (!at.live) return;
-  AttnArgs to;
-  to.out = a.out;
-  to.out_dtype = a.out_dtype;
-  to.out_vec = 1;
-#pragma unroll
-  for (int c = 0; c < 4; ++c)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int d = mine * 128 + c * 32 + i * 8 + half * 4;
-      f32x4 r = f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]} * inv;
-      if (a.norm_weight) r *= *reinterpret_cast<const f32x4*>(a.norm_weight + d);
-      store_out4(to, (row * (a.q_heads / 2) + head) * 256 + d, out_f32x4{r[0], r[1], r[2], r[3]});
-    }
+  write_rows(scratch, o, inv, out_row, 256, mine * 128, a.out, a.out_dtype);
 }
 
 // Adds up the parts of a row: a wave to a row, four channels a lane.

@@ -57,8 +57,9 @@ __device__ __forceinline__ void put_weights(Weights<NP>& w, int ks, int q, float
 // to read, and in the next two each wave waits for its own before it goes on.
 template <bool BF16, int BSC, int NP>
 __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int splits) {
-  __shared__ __attribute__((aligned(16))) u32x4 s_k[kRing][kTilePieces];
-  __shared__ __attribute__((aligned(16))) u32x4 s_v[kRing][kTilePieces];
+  __shared__ __attribute__((aligned(16))) u32x4 s_kv[2][kRing][kTilePieces];
+  auto& s_k = s_kv[0];
+  auto& s_v = s_kv[1];
   __shared__ int s_find[kFindScratch];
   __shared__ int s_bad[129];             // the first token not finite, per channel and of all
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -251,42 +252,25 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
   __syncthreads();
 
   l += other_half(l);
-  if (!at.live) return;
   if (s_bad[128] != INT_MAX)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (at.pos >= s_bad[c * 32 + (i >> 2) * 8 + half * 4 + (i & 3)]) o[c][i] = NAN;
-  const int64_t orow = int64_t(R.row0 + at.tok) * a.q_heads + kvh * G + at.g;
-  if (splits > 1) {
-    const int64_t part = int64_t(split) * a.tokens * a.q_heads + orow;
-    float* po = a.ws + part * 128;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(po + c * 32 + i * 8 + half * 4) =
-            f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
-    if (half == 0) {
-      float* ml = a.ws + int64_t(splits) * a.tokens * a.q_heads * 128 + part * 2;
-      ml[0] = m;
-      ml[1] = l;
-    }
+  const int row = at.live ? (R.row0 + at.tok) * a.q_heads + kvh * G + at.g : -1;
+  u32x4* const scratch = &s_kv[0][0][0] + wave * 512;
+  if (splits == 1) {
+    write_rows(scratch, o, l == 0.0f ? 0.0f : 1.0f / l, row, 128, 0, a.out, a.out_dtype);
     return;
   }
-  AttnArgs to;
-  to.out = a.out;
-  to.out_dtype = a.out_dtype;
-  to.out_vec = 1;
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-#pragma unroll
-  for (int c = 0; c < 4; ++c)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      store_out4(to, orow * 128 + c * 32 + i * 8 + half * 4,
-                 out_f32x4{o[c][4 * i] * inv, o[c][4 * i + 1] * inv, o[c][4 * i + 2] * inv,
-                           o[c][4 * i + 3] * inv});
+  const int64_t rows = int64_t(a.tokens) * a.q_heads;
+  write_rows(scratch, o, 1.0f, row, 128, 0, a.ws + split * rows * 128, kOutF32);
+  if (at.live && half == 0) {
+    float* ml = a.ws + splits * rows * 128 + (split * rows + row) * 2;
+    ml[0] = m;
+    ml[1] = l;
+  }
 }
 
 // Joins the parts of a row: 32 lanes to a row, four channels a lane.

@@ -133,18 +133,19 @@ __device__ __forceinline__ int wave_max(int x) {
   return wave_reduce(x, [](int p, int q) { return max(p, q); });
 }
 
-// Tile `index` of all sequences' tiles, the last tile of every sequence first, then the
-// one before it of those that have two, and so on: the tiles at the end of a
-// long sequence see the most tokens and take the longest, and what is left over at the end
-// of the launch are short ones (four prompts of 257-3841 tokens, sequence by
-// sequence: 246-270 us by their order, so: 240 us). Every wave searches alone, 64 sequences at a time.
+// Tile `index` of all sequences' tiles, those that see the most tokens first (they take
+// the longest, and what is left over at the end of the launch should be short ones):
+// a tile's level is how many tiles of rows its last token lies before the longest
+// sequence's end, so a sequence has one tile at most of each level. (Four prompts of
+// 257-3841 tokens, sequence by sequence: 246-270 us by their order, the last tile of each
+// first: 240, so: 000.) Every wave searches alone, 64 sequences at a time.
 constexpr int kLevelBatch = 512;
 template <int ROWS>
 __device__ __forceinline__ RowTile find_by_level(const PromptArgs& a, int group, int index) {
   constexpr int N = kLevelBatch / 64;
   const int lane = threadIdx.x & 63;
-  int tiles[N], start[N], rows[N], len[N];   // of sequences 64 * i + lane
-  int total = 0, most = 0;
+  int tiles[N], start[N], rows[N], len[N], skip[N];   // of sequences 64 * i + lane
+  int total = 0, longest = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     tiles[i] = rows[i] = start[i] = len[i] = 0;
@@ -156,16 +157,25 @@ __device__ __forceinline__ RowTile find_by_level(const PromptArgs& a, int group,
     }
     tiles[i] = (rows[i] * group + ROWS - 1) / ROWS;
     total += tiles[i];
-    most = max(most, tiles[i]);
+    if (tiles[i] > 0) longest = max(longest, len[i]);
   }
   RowTile r;
   r.b = -1;
   if (index >= wave_sum(total)) return r;
+  longest = wave_max(longest);
+  int most = 0;                          // levels
+#pragma unroll
+  for (int i = 0; i < N; ++i) {          // the level of a sequence's last tile
+    skip[i] = 0;
+    if (i * 64 >= a.batch) continue;
+    skip[i] = min(int64_t(longest - max(len[i], 0)) * group / ROWS, int64_t(1) << 24);
+    if (tiles[i] > 0) most = max(most, skip[i] + tiles[i]);
+  }
   auto below = [&](int level) {          // tiles at levels under this one
     int t = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (i * 64 < a.batch) t += min(tiles[i], level);
+      if (i * 64 < a.batch) t += max(0, min(tiles[i], level - skip[i]));
     return wave_sum(t);
   };
   int lo = 0, hi = wave_max(most), at = 0;     // below(lo) <= index < below(hi)
@@ -178,18 +188,18 @@ __device__ __forceinline__ RowTile find_by_level(const PromptArgs& a, int group,
       hi = mid;
     }
   }
-  int k = index - at;                    // the k-th sequence of more than lo tiles
+  int k = index - at;                    // the k-th sequence with a tile of level lo
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     if (i * 64 >= a.batch || r.b >= 0) continue;
-    const unsigned long long m = __ballot(tiles[i] > lo);
+    const bool has = lo >= skip[i] && lo - skip[i] < tiles[i];
+    const unsigned long long m = __ballot(has);
     const int c = __popcll(m);
     if (k < c) {
-      const unsigned long long hit = __ballot(
-          tiles[i] > lo && __popcll(m & ((1ull << lane) - 1ull)) == k);
+      const unsigned long long hit = __ballot(has && __popcll(m & ((1ull << lane) - 1ull)) == k);
       const int l = __builtin_ctzll(hit);
       r.b = i * 64 + l;
-      r.first = (__builtin_amdgcn_readlane(tiles[i], l) - 1 - lo) * ROWS;
+      r.first = (__builtin_amdgcn_readlane(tiles[i] + skip[i], l) - 1 - lo) * ROWS;
       r.row0 = __builtin_amdgcn_readlane(start[i], l);
       r.n = __builtin_amdgcn_readlane(rows[i], l);
       r.len = __builtin_amdgcn_readlane(len[i], l);
@@ -479,6 +489,57 @@ struct Staging {
     }
   }
 };
+
+// Writes a wave's 32 rows of 128 channels (o: the lane's row lane % 32, channels 32c + 8i +
+// 4 * (lane / 32) + k in o[c][4i + k]) through `lds`, 8 KiB of the wave's own, so that 16
+// lanes store a row's 256 bytes side by side. row: of the output, -1 for none; rows of
+// `row_channels`, the first of them `channel`. Straight from the registers a workgroup took 5 us
+// here, with its compute unit idle.
+__device__ __forceinline__ void write_rows(u32x4* lds, const f32x16 (&o)[4], float by, int row,
+                                           int row_channels, int channel, void* out,
+                                           int out_dtype) {
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int piece = lane & 15;
+  auto store = [&](int bytes) {          // 32 rows of 256 bytes, `bytes` into the output's rows
+#pragma unroll
+    for (int it = 0; it < 8; ++it) {
+      const int r = it * 4 + (lane >> 4);
+      const u32x4 x = lds[r * 16 + (piece ^ (r & 15))];
+      const int to = __shfl(row, r);
+      const int64_t at = int64_t(to) * row_channels + channel;
+      if (to >= 0)
+        *reinterpret_cast<u32x4*>(static_cast<char*>(out) + at * (out_dtype == kOutF32 ? 4 : 2) +
+                                  bytes + piece * 16) = x;
+    }
+  };
+  if (out_dtype == kOutF32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x16& x = o[2 * h + c];
+          lds[col * 16 + ((c * 8 + i * 2 + half) ^ (col & 15))] = __builtin_bit_cast(
+              u32x4, f32x4{x[4 * i] * by, x[4 * i + 1] * by, x[4 * i + 2] * by, x[4 * i + 3] * by});
+        }
+      store(h * 256);
+    }
+    return;
+  }
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = o[c][4 * i] * by, y = o[c][4 * i + 1] * by, z = o[c][4 * i + 2] * by,
+                  w = o[c][4 * i + 3] * by;
+      reinterpret_cast<u32x2*>(lds)[(col * 16 + ((c * 4 + i) ^ (col & 15))) * 2 + half] =
+          out_dtype == kOutBF16 ? u32x2{pack16<true>(x, y), pack16<true>(z, w)}
+                                : u32x2{pack16<false>(x, y), pack16<false>(z, w)};
+    }
+  store(0);
+}
 
 // Order of what the scheduler lays out next, `n` instructions at a time.
 #define EMA_SCHED_VALU(n) __builtin_amdgcn_sched_group_barrier(0x2, n, 0)
