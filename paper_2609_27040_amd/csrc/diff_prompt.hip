@@ -49,6 +49,11 @@ __device__ __forceinline__ void mask_scores(f32x16 (&s)[N], int pos, int t0, int
       s[x][i] = x * 32 + (i >> 3) * 16 + (i & 7) <= rel ? s[x][i] : -INFINITY;
 }
 
+// The first launch leaves (m, l) of every part of a row's tokens side by side, in an even
+// number of places: a row's are then read 16 bytes at a time. (Parts apart, and each lane both
+// maps: 10-14 us of a call of 62 with 21 parts.)
+__host__ __device__ constexpr int stat_room(int splits) { return (splits + 1) & ~1; }
+
 template <bool BF16, int BSC>
 __global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int splits) {
   __shared__ __attribute__((aligned(16))) u32x4 s_k[kRing][kTilePieces];
@@ -166,9 +171,8 @@ __global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int 
   }
   l += other_half(l);
   if (!at.live || half != 0) return;
-  float* ml = a.ws + ((int64_t(split) * a.tokens + R.row0 + at.tok) * a.q_heads + head) * 2;
-  ml[0] = m;
-  ml[1] = l;
+  const int64_t row = int64_t(R.row0 + at.tok) * a.q_heads + head;
+  reinterpret_cast<float2*>(a.ws)[row * stat_room(splits) + split] = float2{m, l};
 }
 
 template <int NP>
@@ -202,32 +206,41 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
   const int head = pair * G + at.g;      // of the output; its maps are query heads 2h, 2h + 1
 
   u32x4 q[2][8];
-  float ref[2], by[2];                   // m, and 1 / l (the second map's times lambda)
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     const char* p = a.q + (row * a.q_stride + (2 * head + x) * 128 + half * 8) * 2;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) q[x][ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
+  }
+  // m, and 1 / l (the second map's times lambda): each half of the wave joins one map's parts
+  float ref[2], by[2];
+  {
+    const f32x4* ml = reinterpret_cast<const f32x4*>(
+        a.ws + (row * a.q_heads + 2 * head + half) * stat_room(stat_splits) * 2);
+    const int n = stat_room(stat_splits) / 2;
     float m = -INFINITY, l = 0.0f;
-    const int64_t step = int64_t(a.tokens) * a.q_heads * 2;
-    const float* ml = a.ws + (row * a.q_heads + 2 * head + x) * 2;
-    for (int y0 = 0; y0 < stat_splits; y0 += 8) {      // eight parts in a round trip
-      float pm[8], pl[8];
+    for (int y0 = 0; y0 < n; y0 += 8) {
+      f32x4 part[8];
 #pragma unroll
-      for (int y = 0; y < 8; ++y) {
-        pm[y] = ml[min(y0 + y, stat_splits - 1) * step];
-        pl[y] = ml[min(y0 + y, stat_splits - 1) * step + 1];
-      }
+      for (int y = 0; y < 8; ++y) part[y] = ml[min(y0 + y, n - 1)];
 #pragma unroll
-      for (int y = 0; y < 8; ++y) {
-        if (y0 + y >= stat_splits) break;
-        const float m_new = fmaxf(m, pm[y]), r = m_new == -INFINITY ? 0.0f : m_new;
-        l = l * __builtin_amdgcn_exp2f(m - r) + pl[y] * __builtin_amdgcn_exp2f(pm[y] - r);
-        m = m_new;
-      }
+      for (int y = 0; y < 8; ++y)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (2 * (y0 + y) + e >= stat_splits) continue;
+          const float pm = part[y][2 * e], pl = part[y][2 * e + 1];
+          const float m_new = fmaxf(m, pm), r = m_new == -INFINITY ? 0.0f : m_new;
+          l = l * __builtin_amdgcn_exp2f(m - r) + pl * __builtin_amdgcn_exp2f(pm - r);
+          m = m_new;
+        }
     }
-    ref[x] = m == -INFINITY ? 0.0f : m;
-    by[x] = l == 0.0f ? 0.0f : (x == 0 ? 1.0f : a.lam[head]) / l;
+    const float mine_ref = m == -INFINITY ? 0.0f : m;
+    const float mine_by = l == 0.0f ? 0.0f : (half == 0 ? 1.0f : a.lam[head]) / l;
+    const float other_ref = other_half(mine_ref), other_by = other_half(mine_by);
+    ref[0] = half == 0 ? mine_ref : other_ref;
+    ref[1] = half == 0 ? other_ref : mine_ref;
+    by[0] = half == 0 ? mine_by : other_by;
+    by[1] = half == 0 ? other_by : mine_by;
   }
 
   const uint32_t lds_k = lds_address(&s_k[0][0][0]), lds_v = lds_address(&s_v[0][0][0]);
@@ -407,7 +420,7 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
   if (splits > 1) {
     const int64_t rows = int64_t(a.tokens) * (a.q_heads / 2);
     write_rows(scratch, o, 1.0f, out_row, 256, mine * 128,
-               a.ws + int64_t(stat_splits) * a.tokens * a.q_heads * 2 + split * rows * 256, kOutF32);
+               a.ws + int64_t(stat_room(stat_splits)) * a.tokens * a.q_heads * 2 + split * rows * 256, kOutF32);
     return;
   }
   float inv = 1.0f;
@@ -443,7 +456,7 @@ __global__ __launch_bounds__(256) void diff_add(PromptArgs a, int stat_splits, i
   const int tok = int(row / (a.q_heads / 2));
   if (tok < a.starts[0] || tok >= a.starts[a.batch]) return;
   const int lane = threadIdx.x & 63;
-  const float* parts = a.ws + int64_t(stat_splits) * a.tokens * a.q_heads * 2;
+  const float* parts = a.ws + int64_t(stat_room(stat_splits)) * a.tokens * a.q_heads * 2;
   f32x4 r = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
   for (int s = 0; s < splits; ++s)
@@ -516,7 +529,7 @@ size_t diff_prompt_workspace(const PromptArgs& a) {
   for (int out : {kOutF32, kOutBF16}) {
     b.out_dtype = out;
     const Cut c = cut_of(b);
-    size_t n = size_t(c.stat_splits) * a.tokens * a.q_heads * 2;
+    size_t n = size_t(stat_room(c.stat_splits)) * a.tokens * a.q_heads * 2;
     if (c.mul_splits > 1) n += size_t(c.mul_splits) * a.tokens * (a.q_heads / 2) * 256;
     most = std::max(most, n);
   }
