@@ -23,6 +23,12 @@ int inval(const char* what, const char* why) {
   return set_error(EMA_ERR_INVAL, std::string(what) + ": " + why);
 }
 
+int32_t log2_of(int32_t x) {   // of a power of two
+  int32_t s = 0;
+  while ((1 << s) < x) ++s;
+  return s;
+}
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 // The host's view of a device array in checked mode, or the caller's own array on
@@ -74,7 +80,7 @@ int tables_sizes(const ema_slice* h, const ema_kv_tables_args* u) {
 }
 
 size_t tables_bytes(const ema_kv_tables_args* u) {
-  const int64_t chunks = ema::table_chunks(u->batch, u->max_blocks);
+  const int64_t chunks = ema::table_chunks(u->layers, u->batch, u->max_blocks);
   return u->staging_slots > 0 && chunks > 1 ? size_t(chunks) * u->layers * 3 * 4 : 0;
 }
 
@@ -183,7 +189,7 @@ ema::PromptArgs kernel_args(const AttnCall& c) {
   a.kv_heads = h->shape.num_kv_heads;
   a.block_size = h->shape.block_size;
   a.max_blocks = c.max_blocks;
-  for (a.block_shift = 0; (1 << a.block_shift) < a.block_size;) ++a.block_shift;
+  a.block_shift = log2_of(a.block_size);
   a.dtype = h->shape.dtype;
   a.out_dtype = c.out_dtype;
   return a;
@@ -314,7 +320,8 @@ int ema_kv_tables(ema_slice_t h, const ema_kv_tables_args* args, void* workspace
   a.n_local = h->book.n_local();
   a.n_total = a.n_local + h->book.n_slice();
   a.block_size = h->shape.block_size;
-  a.chunks = ema::table_chunks(u.batch, u.max_blocks);
+  a.block_shift = log2_of(a.block_size);
+  a.chunks = ema::table_chunks(u.layers, u.batch, u.max_blocks);
   a.counts = static_cast<int32_t*>(workspace);
   a.err_count = h->d_err;
   HIP_TRY(ema::launch_kv_tables(a, st), what);
@@ -369,6 +376,7 @@ int ema_kv_store(ema_slice_t h, const void* k_new, int64_t k_stride, const void*
   a.tokens = tokens;
   a.kv_heads = h->shape.num_kv_heads;
   a.block_size = h->shape.block_size;
+  a.block_shift = log2_of(a.block_size);
   HIP_TRY(ema::launch_kv_store(a, st), what);
   return EMA_OK;
 } catch (...) {

@@ -18,7 +18,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kThreads = 256;
 
 template <int TILE>
-__global__ __launch_bounds__(kThreads) void kv_store_kernel(StoreArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void kv_store_kernel(StoreArgs a) {
   constexpr int kRows = TILE + 7;                    // and what a group reads past the tile
   __shared__ int s_slot[7 + kRows];                  // tokens t0 - 7 .. t0 + TILE + 6
   __shared__ __attribute__((aligned(16))) uint16_t s_v[kRows][128];
@@ -62,19 +62,31 @@ __global__ __launch_bounds__(kThreads) void kv_store_kernel(StoreArgs a) {
       s_n[1] = __popcll(mo);
     }
   }
-  // K rows straight on, V rows into LDS: 16 threads to a row
+  // K rows straight on, V rows into LDS: 16 threads to a row, all their loads at once
   const int piece = tid & 15;
-  for (int i = tid >> 4; i < kRows; i += kThreads / 16) {
-    const int t = t0 + i;
+  constexpr int kRounds = (kRows + kThreads / 16 - 1) / (kThreads / 16);
+  u32x4 kx[kRounds], vx[kRounds];
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int i = (tid >> 4) + r * (kThreads / 16);
+    if (i >= kRows || s_slot[min(i, kRows - 1) + 7] < 0) continue;
+    const int64_t t = t0 + i;
+    vx[r] = __builtin_nontemporal_load(
+        reinterpret_cast<const u32x4*>(a.v + t * a.v_stride + h * 128 + piece * 8));
+    if (i < n)
+      kx[r] = __builtin_nontemporal_load(
+          reinterpret_cast<const u32x4*>(a.k + t * a.k_stride + h * 128 + piece * 8));
+  }
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    const int i = (tid >> 4) + r * (kThreads / 16);
+    if (i >= kRows) continue;
     const int s = s_slot[i + 7];
     if (s < 0) continue;
-    *reinterpret_cast<u32x4*>(&s_v[i][piece * 8]) = __builtin_nontemporal_load(
-        reinterpret_cast<const u32x4*>(a.v + int64_t(t) * a.v_stride + h * 128 + piece * 8));
+    *reinterpret_cast<u32x4*>(&s_v[i][piece * 8]) = vx[r];
     if (i >= n) continue;
-    const u32x4 x = __builtin_nontemporal_load(
-        reinterpret_cast<const u32x4*>(a.k + int64_t(t) * a.k_stride + h * 128 + piece * 8));
-    uint16_t* blk = reinterpret_cast<uint16_t*>(a.local + int64_t(s / BS) * a.block_bytes);
-    *reinterpret_cast<u32x4*>(blk + (int64_t(h) * BS + s % BS) * 128 + piece * 8) = x;
+    uint16_t* blk = reinterpret_cast<uint16_t*>(a.local + int64_t(s >> a.block_shift) * a.block_bytes);
+    *reinterpret_cast<u32x4*>(blk + (int64_t(h) * BS + (s & (BS - 1))) * 128 + piece * 8) = kx[r];
   }
   __syncthreads();
   const int64_t v_half = int64_t(BS) * H * 128;
@@ -87,15 +99,15 @@ __global__ __launch_bounds__(kThreads) void kv_store_kernel(StoreArgs a) {
     uint16_t x[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] = s_v[i + k][d];
-    uint16_t* blk = reinterpret_cast<uint16_t*>(a.local + int64_t(s / BS) * a.block_bytes);
-    *reinterpret_cast<u32x4*>(blk + v_half + (int64_t(h) * 128 + d) * BS + s % BS) =
+    uint16_t* blk = reinterpret_cast<uint16_t*>(a.local + int64_t(s >> a.block_shift) * a.block_bytes);
+    *reinterpret_cast<u32x4*>(blk + v_half + (int64_t(h) * 128 + d) * BS + (s & (BS - 1))) =
         u32x4{x[0] | (uint32_t(x[1]) << 16), x[2] | (uint32_t(x[3]) << 16),
               x[4] | (uint32_t(x[5]) << 16), x[6] | (uint32_t(x[7]) << 16)};
   }
   for (int e = tid; e < s_n[1] * 128; e += kThreads) {
     const int i = s_one[e >> 7], d = e & 127, s = s_slot[i + 7];
-    uint16_t* blk = reinterpret_cast<uint16_t*>(a.local + int64_t(s / BS) * a.block_bytes);
-    blk[v_half + (int64_t(h) * 128 + d) * BS + s % BS] = s_v[i][d];
+    uint16_t* blk = reinterpret_cast<uint16_t*>(a.local + int64_t(s >> a.block_shift) * a.block_bytes);
+    blk[v_half + (int64_t(h) * 128 + d) * BS + (s & (BS - 1))] = s_v[i][d];
   }
 }
 

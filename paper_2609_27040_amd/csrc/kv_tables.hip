@@ -1,7 +1,7 @@
 // Block tables, slot maps and swap lists of a step, from the requests' lengths.
 //
 // A table is walked as one array of batch x max_blocks entries per layer, cut into
-// chunks of kTableChunk entries, one workgroup each. Request b's blocks begin at
+// chunks of 2048 or 4096 entries, one workgroup each. Request b's blocks begin at
 // the prefix sum of the block counts before it, and its new tokens at that of
 // the new lengths: every workgroup adds up the requests before its chunk (a few
 // kilobytes, in cache) and scans its own. The k-th slice block of a layer is staged in
@@ -21,9 +21,15 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) {
   return x < lo ? lo : (x > hi ? hi : x);
 }
 
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+// Inclusive prefix sum over the wave's 64 lanes, by DPP moves: within rows of 16 lanes, then
+// the row totals carried over.
+__device__ __forceinline__ int wave_inclusive_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);    // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // lane 15 of rows 0, 2 to 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2, 3
   return x;
 }
 
@@ -31,11 +37,10 @@ __device__ __forceinline__ int wave_sum(int x) {
 template <int N>
 __device__ __forceinline__ void block_sum(int (&x)[N], int* s) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  __syncthreads();
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const int w = wave_sum(x[n]);
-    if (lane == 0) s[n * kWavesOf + wave] = w;
+    const int w = wave_inclusive_sum(x[n]);
+    if (lane == 63) s[n * kWavesOf + wave] = w;
   }
   __syncthreads();
 #pragma unroll
@@ -60,27 +65,53 @@ __device__ __forceinline__ Lens lens_of(const TablesArgs& a, int b, bool* bad) {
 }
 
 __device__ __forceinline__ int blocks_of(const TablesArgs& a, int len) {
-  return (len + a.block_size - 1) / a.block_size;
+  return (len + a.block_size - 1) >> a.block_shift;
 }
 
-template <bool COUNT>
-__global__ __launch_bounds__(kTableThreads) void kv_tables_kernel(TablesArgs a) {
-  __shared__ int s_first[kTableChunk + 2], s_qs[kTableChunk + 2], s_old[kTableChunk + 2];
-  __shared__ int s_ids[kTableChunk];
-  __shared__ int s_red[6 * kWavesOf];
+template <int ITEMS, bool COUNT>
+// Registers for three workgroups to a CU: with two, large tables take a second round.
+__global__ __launch_bounds__(kTableThreads, 6) void kv_tables_kernel(TablesArgs a) {
+  constexpr int kChunk = kTableThreads * ITEMS;
+  constexpr int kLists = ITEMS == 4 ? kChunk : kChunk / 8 + 1;  // requests of a chunk at most
+  constexpr int kPer = (kLists + kTableThreads - 1) / kTableThreads;
+  __shared__ int s_first[kLists + 2], s_qs[kLists + 2], s_old[kLists + 2];
+  __shared__ int s_ids[kChunk];
+  __shared__ int s_red[9 * kWavesOf];
   __shared__ int s_wave[3][kWavesOf];
   const ema_kv_tables_args& u = a.u;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int chunk = blockIdx.x, layer = blockIdx.y;
   const int B = u.batch, MB = u.max_blocks, BS = a.block_size;
   const int E = B * MB;                    // below 2^31: checked on the host
-  const int e0 = chunk * kTableChunk, e1 = min(E, e0 + kTableChunk);
+  const int e0 = chunk * kChunk, e1 = min(E, e0 + kChunk);
   const int b0 = E ? e0 / MB : 0;
-  const int nloc = E ? (e1 - 1) / MB + 1 - b0 : 0;   // requests of the chunk, at most kTableChunk
+  const int nloc = E ? (e1 - 1) / MB + 1 - b0 : 0;   // requests of the chunk, at most kLists + 1
   const bool staged = u.staging_slots > 0;
 
-  // blocks and new tokens of the requests before the chunk, new tokens of all
-  int sum[3] = {0, 0, 0};
+  // Everything that waits for nothing is sent for at once: the lengths of the chunk's own
+  // requests (thread t takes consecutive ones), the counts of the layer's chunks, and the
+  // lengths of all requests.
+  const int per = (nloc + kTableThreads - 1) / kTableThreads;
+  const int i0 = min(nloc, tid * per), i1 = min(nloc, i0 + per);
+  Lens own[kPer + 1];
+#pragma unroll
+  for (int i = 0; i <= kPer; ++i) {
+    own[i] = Lens{0, 0};
+    bool bad;
+    if (i0 + i < i1) own[i] = lens_of(a, b0 + i0 + i, &bad);
+  }
+  // 0: blocks, 1: new tokens of the requests before the chunk; 2: new tokens of all; of the
+  // layer's slice blocks, prefetches and write-backs, 3-5: those before the chunk, 6-8: all
+  int sum[9] = {};
+  if (!COUNT && staged && a.chunks > 1)
+    for (int c = tid; c < a.chunks; c += kTableThreads) {
+#pragma unroll
+      for (int x = 0; x < 3; ++x) {
+        const int v = a.counts[(int64_t(layer) * a.chunks + c) * 3 + x];
+        sum[6 + x] += v;
+        if (c < chunk) sum[3 + x] += v;
+      }
+    }
   for (int b = tid; b < B; b += kTableThreads) {
     bool bad;
     const Lens l = lens_of(a, b, &bad);
@@ -91,63 +122,49 @@ __global__ __launch_bounds__(kTableThreads) void kv_tables_kernel(TablesArgs a) 
     }
     sum[2] += l.fresh;
   }
-  block_sum(sum, s_red);
-  const int total_new = sum[2];
-
-  // the chunk's own requests: thread t takes consecutive ones
-  {
-    const int per = (nloc + kTableThreads - 1) / kTableThreads;
-    const int i0 = min(nloc, tid * per), i1 = min(nloc, i0 + per);
-    int nb = 0, nf = 0;
-    for (int i = i0; i < i1; ++i) {
-      bool bad;
-      const Lens l = lens_of(a, b0 + i, &bad);
-      nb += blocks_of(a, l.len);
-      nf += l.fresh;
-      s_old[i] = l.len - l.fresh;
-    }
-    int ib = nb, jf = nf;                   // inclusive over the wave
+  int nb = 0, nf = 0;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(ib, o), y = __shfl_up(jf, o);
-      if (lane >= o) {
-        ib += x;
-        jf += y;
-      }
-    }
-    if (lane == 63) {
-      s_wave[0][wave] = ib;
-      s_wave[1][wave] = jf;
-    }
-    __syncthreads();
+  for (int i = 0; i <= kPer; ++i) {
+    nb += blocks_of(a, own[i].len);
+    nf += own[i].fresh;
+    if (i0 + i < i1) s_old[i0 + i] = own[i].len - own[i].fresh;
+  }
+  const int ib = wave_inclusive_sum(nb), jf = wave_inclusive_sum(nf);
+  if (lane == 63) {
+    s_wave[0][wave] = ib;
+    s_wave[1][wave] = jf;
+  }
+  block_sum(sum, s_red);                    // also makes s_wave visible
+  const int total_new = sum[2];
+  {
     int at_b = sum[0] + ib - nb, at_f = sum[1] + jf - nf;
     for (int w = 0; w < wave; ++w) {
       at_b += s_wave[0][w];
       at_f += s_wave[1][w];
     }
-    for (int i = i0; i < i1; ++i) {
-      bool bad;
-      const Lens l = lens_of(a, b0 + i, &bad);
-      s_first[i] = at_b;
-      s_qs[i] = at_f;
-      at_b += blocks_of(a, l.len);
-      at_f += l.fresh;
-      if (i == nloc - 1) {
+#pragma unroll
+    for (int i = 0; i <= kPer; ++i) {
+      if (i0 + i >= i1) continue;
+      s_first[i0 + i] = at_b;
+      s_qs[i0 + i] = at_f;
+      at_b += blocks_of(a, own[i].len);
+      at_f += own[i].fresh;
+      if (i0 + i == nloc - 1) {
         s_first[nloc] = at_b;
         s_qs[nloc] = at_f;
       }
     }
     if (nloc == 0 && tid == 0) s_qs[0] = 0;
-    __syncthreads();
   }
+  __syncthreads();
 
-  // the entries: wave w takes kTableItems runs of 64 consecutive ones
-  int id[kTableItems], rank[kTableItems][3];
-  bool is[kTableItems][3];                 // in the slice; to prefetch; to write back
+  // the entries: wave w takes ITEMS runs of 64 consecutive ones
+  int id[ITEMS], rank[ITEMS][3];
+  bool is[ITEMS][3];                 // in the slice; to prefetch; to write back
   int n[3] = {0, 0, 0};
 #pragma unroll
-  for (int k = 0; k < kTableItems; ++k) {
-    const int e = e0 + (wave * kTableItems + k) * 64 + lane;
+  for (int k = 0; k < ITEMS; ++k) {
+    const int e = e0 + (wave * ITEMS + k) * 64 + lane;
     id[k] = -1;
     bool away = false, older = false, touched = false;
     if (e < e1) {
@@ -190,33 +207,22 @@ __global__ __launch_bounds__(kTableThreads) void kv_tables_kernel(TablesArgs a) 
   }
 
   if (staged) {
-    int tot[6] = {0, 0, 0, 0, 0, 0};       // before this chunk, in the layer
-    if (a.chunks > 1) {
-      for (int c = tid; c < a.chunks; c += kTableThreads) {
-#pragma unroll
-        for (int x = 0; x < 3; ++x) {
-          const int v = a.counts[(int64_t(layer) * a.chunks + c) * 3 + x];
-          tot[3 + x] += v;
-          if (c < chunk) tot[x] += v;
-        }
-      }
-      block_sum(tot, s_red);
-    } else {
+    if (a.chunks == 1) {
 #pragma unroll
       for (int x = 0; x < 3; ++x)
-        for (int w = 0; w < kWavesOf; ++w) tot[3 + x] += s_wave[x][w];
+        for (int w = 0; w < kWavesOf; ++w) sum[6 + x] += s_wave[x][w];
     }
     int base[3];
 #pragma unroll
     for (int x = 0; x < 3; ++x) {
-      base[x] = tot[x];
+      base[x] = sum[3 + x];
       for (int w = 0; w < wave; ++w) base[x] += s_wave[x][w];
     }
     const int64_t pl = int64_t(layer) * u.stage_n, wl = int64_t(layer) * u.writeback_cap;
     const int32_t* places = u.staging_ids + int64_t(layer % u.staging_slots) * u.stage_n;
 #pragma unroll
-    for (int k = 0; k < kTableItems; ++k) {
-      const int e = e0 + (wave * kTableItems + k) * 64 + lane;
+    for (int k = 0; k < ITEMS; ++k) {
+      const int e = e0 + (wave * ITEMS + k) * 64 + lane;
       int entry = id[k];
       if (is[k][0]) {
         const int r = base[0] + rank[k][0];
@@ -246,7 +252,7 @@ __global__ __launch_bounds__(kTableThreads) void kv_tables_kernel(TablesArgs a) 
         s_ids[e - e0] = entry;
       }
     }
-    const int n_pf = min(tot[4], u.stage_n), n_wb = min(tot[5], u.writeback_cap);
+    const int n_pf = min(sum[7], u.stage_n), n_wb = min(sum[8], u.writeback_cap);
     if (chunk == 0 && tid == 0) {
       u.prefetch_n[layer] = n_pf;
       u.writeback_n[layer] = n_wb;
@@ -260,8 +266,8 @@ __global__ __launch_bounds__(kTableThreads) void kv_tables_kernel(TablesArgs a) 
       u.writeback_src[wl + p] = u.writeback_dst[wl + p] = -1;
   } else {
 #pragma unroll
-    for (int k = 0; k < kTableItems; ++k) {
-      const int e = e0 + (wave * kTableItems + k) * 64 + lane;
+    for (int k = 0; k < ITEMS; ++k) {
+      const int e = e0 + (wave * ITEMS + k) * 64 + lane;
       if (e >= e1) continue;
       const int64_t at = int64_t(layer) * E + e;
       u.block_table[at] = id[k];
@@ -286,7 +292,7 @@ __global__ __launch_bounds__(kTableThreads) void kv_tables_kernel(TablesArgs a) 
       const int mid = (lo + hi) >> 1;
       if (s_qs[mid] <= t) lo = mid; else hi = mid;
     }
-    const int p = s_old[lo] + t - s_qs[lo], j = p / BS;
+    const int p = s_old[lo] + t - s_qs[lo], j = p >> a.block_shift;
     const int v = s_ids[(b0 + lo) * MB + j - e0];
     const bool ok = v >= 0 && v < a.n_local;
     if (!ok || t >= u.n_slots) atomicAdd(a.err_count, 1);
@@ -304,16 +310,26 @@ __global__ __launch_bounds__(kTableThreads) void kv_tables_kernel(TablesArgs a) 
 
 }  // namespace
 
-hipError_t launch_kv_tables(const TablesArgs& a, hipStream_t stream) {
-  if (a.u.layers == 0) return hipSuccess;
+namespace {
+
+template <int ITEMS>
+hipError_t launch(const TablesArgs& a, hipStream_t stream) {
   const dim3 grid(a.chunks, a.u.layers);
   if (a.chunks > 1 && a.u.staging_slots > 0) {
-    hipLaunchKernelGGL(kv_tables_kernel<true>, grid, dim3(kTableThreads), 0, stream, a);
+    hipLaunchKernelGGL((kv_tables_kernel<ITEMS, true>), grid, dim3(kTableThreads), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kv_tables_kernel<false>, grid, dim3(kTableThreads), 0, stream, a);
+  hipLaunchKernelGGL((kv_tables_kernel<ITEMS, false>), grid, dim3(kTableThreads), 0, stream, a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv_tables(const TablesArgs& a, hipStream_t stream) {
+  if (a.u.layers == 0) return hipSuccess;
+  return table_items(a.u.layers, a.u.batch, a.u.max_blocks) == 4 ? launch<4>(a, stream)
+                                                                : launch<8>(a, stream);
 }
 
 }  // namespace ema

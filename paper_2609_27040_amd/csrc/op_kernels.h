@@ -13,20 +13,26 @@ namespace ema {
 // ---- tables ------------------------------------------------------------------------
 
 constexpr int kTableThreads = 512;
-constexpr int kTableItems = 4;
-constexpr int kTableChunk = kTableThreads * kTableItems;   // table entries of a workgroup
 
+// Table entries that a thread takes, and with it a workgroup. Eight where there are enough of
+// them for 512 workgroups and the rows are not too short for a workgroup's list of its
+// requests, else four, so that small tables still spread over the chip. 80 layers of 128
+// requests of up to 504 blocks, us a call with four / eight / sixteen: 66 / 49 / 51.
+inline int32_t table_items(int64_t layers, int64_t batch, int64_t max_blocks) {
+  return max_blocks >= 8 && layers * batch * max_blocks >= 512 * kTableThreads * 8 ? 8 : 4;
+}
+inline int32_t table_chunks(int64_t layers, int64_t batch, int64_t max_blocks) {
+  const int64_t chunk = kTableThreads * table_items(layers, batch, max_blocks);
+  const int64_t n = (batch * max_blocks + chunk - 1) / chunk;
+  return int32_t(n > 0 ? n : 1);
+}
 struct TablesArgs {
   ema_kv_tables_args u;
-  int32_t n_local, n_total, block_size;
+  int32_t n_local, n_total, block_size, block_shift;
   int32_t chunks;        // workgroups of a layer
   int32_t* counts;       // [layers][chunks][3] slice, prefetch and write-back entries
   int32_t* err_count;
 };
-inline int32_t table_chunks(int64_t batch, int64_t max_blocks) {
-  const int64_t n = (batch * max_blocks + kTableChunk - 1) / kTableChunk;
-  return int32_t(n > 0 ? n : 1);
-}
 hipError_t launch_kv_tables(const TablesArgs& a, hipStream_t stream);
 
 // ---- store --------------------------------------------------------------------------
@@ -41,6 +47,7 @@ struct StoreArgs {
   int64_t block_bytes;
   int32_t n_slots;              // rows of the local pool
   int32_t tokens, kv_heads, block_size;
+  int32_t block_shift;          // log2(block_size)
 };
 hipError_t launch_kv_store(const StoreArgs& a, hipStream_t stream);
 

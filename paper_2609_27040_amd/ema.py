@@ -165,6 +165,7 @@ class _Torch:
         self.out_codes = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
         self.out_types = tuple(self.out_codes)
         self.i32 = (torch.int32,)
+        self.f32 = (torch.float32,)
         self.kv16 = {F16: (torch.float16,), BF16: (torch.bfloat16,)}
         self.any16 = (torch.float16, torch.bfloat16, torch.int16)
         raw, dev = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream",
@@ -446,43 +447,43 @@ def _scratch(nbytes, workspace, stream, device):
     return workspace, _dev(workspace, "workspace", (workspace.dtype,)), n
 
 
-def _i32_out(t, name, host, shape):
-    """An int32 array of exactly this shape."""
-    if tuple(t.shape) != tuple(shape):
-        _bad(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+def _i32_exact(t, name, host, shape):
+    """Address of an int32 array of exactly this shape."""
+    if t.shape != shape:
+        _bad(f"{name}: shape {tuple(t.shape)}, expected {shape}")
     if host:
         if not isinstance(t, np.ndarray) or t.dtype != np.int32 or not t.flags.c_contiguous:
             _bad(f"{name}: expected a contiguous int32 numpy array")
         return t.ctypes.data
-    return _i32_dev(t, name)
+    return _dev(t, name, _torch().i32)
 
 
-def _tables_args(h, block_ids, seq_lens, new_lens, block_table, slot_map, query_start, canon_table,
-                 staging, prefetch, writeback):
-    host = _host_only(h)
-    L, B, max_blocks = (int(x) for x in block_table.shape)
-    a = KVTablesArgs(layers=L, batch=B, max_blocks=max_blocks, n_ids=int(block_ids.shape[-1]),
-                     n_slots=int(slot_map.shape[-1]))
-    put = lambda field, t, shape: setattr(a, field, _i32_out(t, field, host, shape))
-    put("block_ids", block_ids, (L, a.n_ids))
-    put("seq_lens", seq_lens, (B,))
-    put("new_lens", new_lens, (B,))
-    put("block_table", block_table, (L, B, max_blocks))
-    put("query_start", query_start, (B + 1,))
-    put("slot_map", slot_map, (L, a.n_slots))
-    if canon_table is not None:
-        put("canon_table", canon_table, (L, B, max_blocks))
+def _tables_args(host, block_ids, seq_lens, new_lens, block_table, slot_map, query_start,
+                 canon_table, staging, prefetch, writeback):
+    L, B, max_blocks = block_table.shape
+    n_ids, n_slots = block_ids.shape[-1], slot_map.shape[-1]
+    addr = [_i32_exact(block_ids, "block_ids", host, (L, n_ids)),
+            _i32_exact(seq_lens, "seq_lens", host, (B,)),
+            _i32_exact(new_lens, "new_lens", host, (B,)), None,
+            None if canon_table is None else
+            _i32_exact(canon_table, "canon_table", host, (L, B, max_blocks)),
+            _i32_exact(block_table, "block_table", host, (L, B, max_blocks)),
+            _i32_exact(query_start, "query_start", host, (B + 1,)),
+            _i32_exact(slot_map, "slot_map", host, (L, n_slots))]
+    slots = stage_n = cap = 0
     if staging is not None:
         if prefetch is None or writeback is None:
             _bad("staging needs the prefetch and writeback lists")
-        a.staging_slots, a.stage_n = (int(x) for x in staging.shape)
-        a.writeback_cap = int(writeback[0].shape[-1])
-        put("staging_ids", staging, (a.staging_slots, a.stage_n))
-        for kind, lists, n in (("prefetch", prefetch, a.stage_n),
-                               ("writeback", writeback, a.writeback_cap)):
-            for end, t, shape in zip(("src", "dst", "n"), lists, ((L, n), (L, n), (L,))):
-                put(f"{kind}_{end}", t, shape)
-    return a
+        slots, stage_n = staging.shape
+        cap = writeback[0].shape[-1]
+        addr[3] = _i32_exact(staging, "staging", host, (slots, stage_n))
+        for kind, (src, dst, count), n in (("prefetch", prefetch, stage_n),
+                                           ("writeback", writeback, cap)):
+            addr += [_i32_exact(src, kind, host, (L, n)), _i32_exact(dst, kind, host, (L, n)),
+                     _i32_exact(count, kind, host, (L,))]
+    else:
+        addr += [None] * 6
+    return KVTablesArgs(*addr, L, B, max_blocks, n_ids, n_slots, slots, stage_n, cap)
 
 
 def kv_tables_workspace(h, args):
@@ -502,30 +503,36 @@ def kv_tables(h, block_ids, seq_lens, new_lens, block_table, slot_map, query_sta
     and ``prefetch`` (src [L][stage_n], dst, count [L]) and ``writeback`` (src
     [L][cap], dst, count [L]) are written. int32 device tensors (numpy arrays for
     a host-only slice, which only validates)."""
-    a = _tables_args(h, block_ids, seq_lens, new_lens, block_table, slot_map, query_start,
+    rec = _HANDLES.get(h)
+    host = rec[0] if rec else _host_only(h)
+    a = _tables_args(host, block_ids, seq_lens, new_lens, block_table, slot_map, query_start,
                      canon_table, staging, prefetch, writeback)
-    if _host_only(h):
+    if host:
         _check(_lib.ema_kv_tables(h, ctypes.byref(a), None, 0, None))
         return
     st = _stream(stream)
-    ws, p, n = _scratch(kv_tables_workspace(h, a), workspace, st, block_table.device)
+    size = 0 if staging is None else kv_tables_workspace(h, a)
+    ws, p, n = _scratch(size, workspace, st, block_table.device)
     _check(_lib.ema_kv_tables(h, ctypes.byref(a), p, n, st))
 
 
-def _rows16(t, name, rec, heads):
+def _rows16(t, name, types, heads):
     """(address, elements between tokens) of a 16-bit GPU tensor [T][heads][128]
     whose tokens may lie apart."""
-    T = _torch()
-    if not isinstance(t, T.Tensor) or not t.is_cuda:
+    if not isinstance(t, _torch().Tensor) or not t.is_cuda:
         _bad(f"{name}: expected a GPU tensor, got {type(t).__name__}")
-    if t.dtype not in _kv16_types(rec):
-        _bad(f"{name}: dtype {t.dtype} not in {_kv16_types(rec)}")
-    if t.dim() != 3 or t.shape[2] != 128 or (heads and t.shape[1] != heads):
-        _bad(f"{name}: shape {tuple(t.shape)}, expected [tokens][{heads or 'heads'}][128]")
+    if t.dtype not in types:
+        _bad(f"{name}: dtype {t.dtype} not in {types}")
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != 128 or (heads and shape[1] != heads):
+        _bad(f"{name}: shape {tuple(shape)}, expected [tokens][{heads or 'heads'}][128]")
+    row = shape[1] * 128
+    if t.is_contiguous():
+        return t.data_ptr(), row
     stride = t.stride()
-    if t.numel() and (stride[2] != 1 or (t.shape[1] > 1 and stride[1] != 128)):
+    if stride[2] != 1 or (shape[1] > 1 and stride[1] != 128):
         _bad(f"{name}: a token's heads are not contiguous")
-    return t.data_ptr(), (int(stride[0]) if t.shape[0] > 1 else int(t.shape[1]) * 128)
+    return t.data_ptr(), stride[0] if shape[0] > 1 else row
 
 
 def kv_store(h, k_new, v_new, slot_map, stream=None):
@@ -538,10 +545,10 @@ def kv_store(h, k_new, v_new, slot_map, stream=None):
         _check(_lib.ema_kv_store(h, None, row, None, row, slots.ctypes.data, len(slots), None))
         return
     rec = _HANDLES.get(h)
-    heads = rec[2] if rec else 0
-    k, ks = _rows16(k_new, "k_new", rec, heads)
-    v, vs = _rows16(v_new, "v_new", rec, heads)
-    T = int(k_new.shape[0])
+    heads, types = rec[2] if rec else 0, _kv16_types(rec)
+    k, ks = _rows16(k_new, "k_new", types, heads)
+    v, vs = _rows16(v_new, "v_new", types, heads)
+    T = k_new.shape[0]
     if v_new.shape != k_new.shape:
         _bad(f"v_new: shape {tuple(v_new.shape)}, k_new has {tuple(k_new.shape)}")
     if slot_map.numel() != T:
@@ -553,33 +560,31 @@ def kv_store(h, k_new, v_new, slot_map, stream=None):
 def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out, scale, lam,
                   norm_weight, norm_eps, workspace, stream):
     T = _torch()
-    rows, Hq = int(q.shape[0]), int(q.shape[1])
+    rows, Hq = q.shape[0], q.shape[1]
     if len(block_table.shape) != 2:
         _bad("block_table: expected [batch][max_blocks]")
-    B, max_blocks = int(block_table.shape[0]), int(block_table.shape[1])
+    B, max_blocks = block_table.shape
     extra = () if maps == 1 else (None, None, float(norm_eps))
     sizes = (rows, B, Hq, max_blocks) if query_start is not None else (B, Hq, max_blocks)
     if query_start is None and rows != B:
         _bad(f"q: {rows} rows, {B} sequences")
-    if _host_only(h):
+    rec = _HANDLES.get(h)
+    if rec[0] if rec else _host_only(h):
         table, lens = _i32_host(block_table), _i32_host(seq_lens)
         starts = () if query_start is None else (_i32_host(query_start).ctypes.data,)
         _check(fn(h, None, Hq * 128, *starts, table.ctypes.data, lens.ctypes.data, *sizes,
                   float(scale), *extra, None, F32, None, 0, None))
         return
-    rec = _HANDLES.get(h)
     code = T.out_codes.get(out.dtype)
     if code is None:
         _bad(f"out: dtype {out.dtype} not in {T.out_types}")
-    qp, qs = _rows16(q, "q", rec, 0)
+    qp, qs = _rows16(q, "q", _kv16_types(rec), 0)
     starts = () if query_start is None else (_i32_dev(query_start, "query_start", B + 1),)
     table = _i32_dev(block_table, "block_table", B * max_blocks)
     lens = _i32_dev(seq_lens, "seq_lens", B)
     if maps == 2:
-        import torch
-        f32 = (torch.float32,)
-        extra = (_dev(lam, "lam", f32, Hq // 2),
-                 None if norm_weight is None else _dev(norm_weight, "norm_weight", f32, 256),
+        extra = (_dev(lam, "lam", T.f32, Hq // 2),
+                 None if norm_weight is None else _dev(norm_weight, "norm_weight", T.f32, 256),
                  float(norm_eps))
     dst = _dev(out, "out", T.out_types, rows * Hq * 128)
     st = _stream(stream)
