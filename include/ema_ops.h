@@ -50,7 +50,9 @@ extern "C" {
  *   writeback_src/dst[l]  staged copies and slice ids of the slice blocks that
  *                         take new tokens, in order, what ema_slice_writeback
  *                         takes; writeback_n[l] of them, -1 behind
- *                         (writeback_cap entries a layer)
+ *                         (writeback_cap entries a layer). A block without older
+ *                         tokens was not prefetched: behind the request's length
+ *                         it takes back whatever its staging block held
  * All arrays are device int32, written whole. Without staging (staging_slots
  * 0) block_table keeps slice ids, the lists are not touched and their pointers may be
  * NULL. The outputs must not overlap each other or the inputs. Lengths outside

@@ -15,6 +15,10 @@ memory (section 3, local-remote symmetry).
 block lives either locally in every layer or at one slab position (every
 layer); the swap of a layer group copies whole slab runs into a staging image.
 
+``Chunk`` holds the tables of a step in which sequences gain several tokens at
+once (prompts): ``PagedKVCache.chunk`` has them built on the GPU, and the cache's
+``store``, ``prompt_attention`` and ``diff_prompt_attention`` go by them.
+
 Both expose the same step interface (``groups``, ``group``, ``staging_slots``,
 ``prefetch_group``, ``attention``), which ``step.StepRunner`` drives.
 """
@@ -28,6 +32,38 @@ TORCH_DT = {"f16": torch.float16, "bf16": torch.bfloat16}
 
 def _dev(a):
     return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to("cuda")
+
+
+class Chunk:
+    """The tables of one step of a ``PagedKVCache`` whose sequences' last
+    ``new_lens`` tokens are new, for all layers, on the device: ``starts`` [B + 1],
+    ``slots`` [L][T], ``block_table`` [L][B][max_blocks] (slice blocks named by
+    their staged copies), and per layer the lists of the slice blocks to prefetch
+    (those that hold older tokens) and to write back (those that take new ones),
+    whose lengths are host ints."""
+
+    def __init__(self, cache, new_lens, stream=None):
+        self.new = np.asarray(new_lens, dtype=np.int64)
+        self.T = int(self.new.sum())
+        L, B, width = cache.tables.shape
+        nblk = -(-cache.lens // cache.bs)
+        used = np.arange(width)[None, :] < nblk[:, None]
+        ids = cache.tables[:, used]                             # (b, j) order
+        away = cache.tables >= cache.n_local
+        j = np.arange(width)[None, :]
+        old = (cache.lens - self.new)[:, None]
+        self.n_prefetch = (away & (j * cache.bs < old)).sum(axis=(1, 2)).tolist()
+        touched = ((j + 1) * cache.bs > old) & (self.new[:, None] > 0)
+        self.n_writeback = (away & touched).sum(axis=(1, 2)).tolist()
+        i32 = dict(dtype=torch.int32, device="cuda")
+        self.block_table = torch.empty((L, B, width), **i32)
+        self.slots = torch.empty((L, self.T), **i32)
+        self.starts = torch.empty(B + 1, **i32)
+        new_list = lambda n: tuple(torch.empty(s, **i32) for s in ((L, n), (L, n), (L,)))
+        self.prefetch, self.writeback = new_list(cache.stage_n), new_list(max(self.n_writeback))
+        ema.kv_tables(cache.h, _dev(ids), cache.lens_dev, _dev(self.new), self.block_table,
+                      self.slots, self.starts, staging=_dev(cache.staging),
+                      prefetch=self.prefetch, writeback=self.writeback, stream=stream)
 
 
 class PagedKVCache:
@@ -160,6 +196,39 @@ class PagedKVCache:
     def attention(self, l, out, table=None, stream=None):
         ema.paged_decode_attention(self.h, self.q, self.attn_dev[l] if table is None else table,
                                    self.lens_dev, out, stream=stream)
+
+    # ---- chunks of prompts ---------------------------------------------------------------
+    def chunk(self, new_lens, stream=None):
+        """The tables of a step that brings each sequence's last new_lens tokens
+        (``self.lens`` counts them already; their blocks are allocated)."""
+        return Chunk(self, new_lens, stream)
+
+    def prefetch_chunk(self, l, chunk, stream=None):
+        ema.slice_prefetch(self.h, chunk.prefetch[0][l], chunk.prefetch[1][l],
+                           chunk.n_prefetch[l], stream=stream)
+
+    def store(self, l, chunk, k_new, v_new, stream=None):
+        """The chunk's K and V [T][Hkv][D] into layer l's blocks."""
+        ema.kv_store(self.h, k_new, v_new, chunk.slots[l], stream=stream)
+
+    def prompt_attention(self, l, chunk, q, out, stream=None):
+        ema.paged_prompt_attention(self.h, q, chunk.starts, chunk.block_table[l], self.lens_dev,
+                                   out, stream=stream)
+
+    def diff_prompt_attention(self, l, chunk, q, lam, out, stream=None, **norm):
+        ema.paged_diff_prompt_attention(self.h, q, chunk.starts, chunk.block_table[l],
+                                        self.lens_dev, lam, out, stream=stream, **norm)
+
+    def diff_attention(self, l, q, lam, out, stream=None, **norm):
+        """Differential attention of one token per sequence, over the tables of a
+        decode step (``restage``)."""
+        ema.paged_diff_attention(self.h, q, self.attn_dev[l], self.lens_dev, lam, out,
+                                 stream=stream, **norm)
+
+    def writeback_chunk(self, l, chunk, stream=None):
+        """The staged copies that took the chunk's tokens, back to the slice."""
+        ema.slice_writeback(self.h, chunk.writeback[0][l], chunk.writeback[1][l],
+                            chunk.n_writeback[l], stream=stream)
 
     def new_token_kv(self, seed=0):
         """One new token's K and V per sequence (device, the cache dtype),

@@ -5,7 +5,8 @@ swaps the group's slice-resident blocks into a staging area, then paged
 decode attention runs for each of the group's layers (section 2.3: a layer is
 not needed again until every other layer has run, which is the window the
 swap of the next group overlaps; section 4.2.2: swaps are issued at layer
-group boundaries into a swap buffer of one group). ``capture_ops`` and
+group boundaries into a swap buffer of one group). ``run_chunk`` orders a step
+that brings many tokens of a sequence at once. ``capture_ops`` and
 ``capture_step`` record a one-stream step as a HIP graph. ``BlockedTimer``
 times a library call that also does host work.
 """
@@ -147,6 +148,22 @@ class StepRunner:
                 # the group's modified staged copies go back before its slots are refilled
                 s2.wait_event(self.ev_at[groups[u][-1]])
                 w.writeback_group(u, stream=s2)
+
+
+def run_chunk(w, chunk, layer, stream=None):
+    """One step of a paged cache that brings a chunk of new tokens (``w.chunk``):
+    layer by layer, the slice blocks that hold older tokens are prefetched,
+    ``layer(l)`` gives the layer's (q, k_new, v_new, out), the new K and V are stored,
+    attention reads the chunk's rows against everything before them, and the staged copies that
+    took tokens go back to the slice. A layer's staging slot is used again
+    ``w.staging_slots`` layers later, behind its write-back on the same stream.
+    Only queues work, so a step whose tensors stay in place can be captured."""
+    for l in range(w.L):
+        w.prefetch_chunk(l, chunk, stream=stream)
+        q, k_new, v_new, out = layer(l)
+        w.store(l, chunk, k_new, v_new, stream=stream)
+        w.prompt_attention(l, chunk, q, out, stream=stream)
+        w.writeback_chunk(l, chunk, stream=stream)
 
 
 def capture_ops(runner, ops):

@@ -569,3 +569,113 @@ def test_checked_handles_read_the_arrays_back(ema):
         del g
     finally:
         c.close()
+
+
+# ---- larger grids, batches and pools -------------------------------------------------------
+
+def test_tables_large_enough_for_the_larger_chunks(ema):
+    L, B, width, bs = 3, 1000, 720, 16
+    rng = np.random.default_rng(40)
+    lens = rng.integers(0, 700, B)
+    lens[[0, 500, 999]] = [width * bs, 0, width * bs - 5]
+    new = np.minimum(lens, rng.integers(0, 40, B))
+    new[0] = 3000
+    ids, staging, n_local, n_slice = table_case(rng, L, lens, new, bs, 0.4, 2)
+    bb = 2 * bs * D * 2
+    h = ema.slice_create(1, D, bs, "bf16", 0, n_local * bb, n_slice * bb)
+    try:
+        T, cap = int(new.sum()), int((-(-new // bs) + 1).sum())
+        o = TableOuts(L, B, width, T, staging.shape[1], cap)
+        run_tables(ema, h, ids, lens, new, o, staging)
+        assert_tables(o, oops.kv_tables(ids, lens, new, width, bs, n_local, T, staging, cap),
+                      staging)
+        assert ema.slice_device_errors(h) == 0
+    finally:
+        ema.slice_destroy(h)
+
+
+@pytest.mark.parametrize("maps,out", [(1, "bf16"), (1, "f32"), (2, "bf16"), (2, "f32")])
+def test_more_sequences_than_a_wave_searches(ema, maps, out):
+    rng = np.random.default_rng(41)
+    lens = rng.integers(0, 40, 700)
+    lens[[3, 699]] = [400, 333]
+    new = np.minimum(lens, rng.integers(0, 6, 700))
+    new[[3, 699]] = [150, 40]
+    c = SmallCache(ema, lens, 2, 16, "bf16", seed=41, extra_width=0)
+    try:
+        check_attention(ema, c, new.tolist(), 4, out, maps, pad=1)
+        assert ema.slice_device_errors(c.h) == 0
+    finally:
+        c.close()
+
+
+def test_differential_decode_of_more_pairs_than_workgroups(ema):
+    rng = np.random.default_rng(42)
+    lens = rng.integers(0, 300, 350)
+    lens[[0, 7, 200, 349]] = [3000, 0, 1700, 33]
+    c = SmallCache(ema, lens, 2, 16, "f16", seed=42)
+    try:
+        check_attention(ema, c, [1] * 350, 4, "f32", 2, single=True)
+        check_attention(ema, c, [1] * 350, 2, "f16", 2, norm=True, single=True)
+        assert ema.slice_device_errors(c.h) == 0
+    finally:
+        c.close()
+
+
+def test_blocks_past_four_gibibytes(ema):
+    """A pool of 5 GiB whose last blocks are used: offsets take more than 32 bits."""
+    H, bs, n = 8, 256, 5120                              # blocks of 1 MiB
+    bb = 2 * bs * H * D * 2
+    small = SmallCache(ema, [600, 300], H, bs, "bf16", seed=43, spare=0)
+    h = ema.slice_create(H, D, bs, "bf16", 0, n * bb, 0)
+    try:
+        view = ema.pool_view(h, ema.POOL_LOCAL)
+        first = n - small.n_local
+        view[first:].copy_(small.view)
+        table = i32(np.where(small.table >= 0, small.table + first, -1))
+        q = dev16(small.queries(40, 16), "bf16")
+        k, v = (dev16(small.queries(3, H), "bf16") for _ in range(2))
+        slots = np.array([5, 70, 511]) + (small.table[1, 0] * bs)
+        lam = torch.linspace(0.1, 0.9, 8, device="cuda")
+        starts, one = i32([0, 30, 40]), q[:2].contiguous()
+        got = []
+        for hh, t, s in ((small.h, small.table_dev, slots), (h, table, slots + first * bs)):
+            ok = i32(np.where(slots // bs == small.table[1, 0], s, -1))
+            ema.kv_store(hh, k, v, ok)
+            outs = [torch.zeros((40, 16, D), dtype=torch.bfloat16, device="cuda"),
+                    torch.zeros((40, 8, 2 * D), dtype=torch.bfloat16, device="cuda"),
+                    torch.zeros((2, 8, 2 * D), dtype=torch.bfloat16, device="cuda")]
+            ema.paged_prompt_attention(hh, q, starts, t, small.lens_dev, outs[0])
+            ema.paged_diff_prompt_attention(hh, q, starts, t, small.lens_dev, lam, outs[1])
+            ema.paged_diff_attention(hh, one, t, small.lens_dev, lam, outs[2])
+            torch.cuda.synchronize()
+            got.append(outs)
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+        assert torch.equal(view[first:], small.view)
+        view = None
+    finally:
+        view = None
+        small.close()
+        ema.slice_destroy(h)
+
+
+def test_results_do_not_depend_on_placement_or_width(ema):
+    """The same tokens in other blocks and a wider table: the same bits (the width decides how
+    the work is cut only where rows are few)."""
+    a = SmallCache(ema, [700, 90], 2, 16, "bf16", seed=44)
+    b = SmallCache(ema, [700, 90], 2, 16, "bf16", seed=44, spare=3)
+    try:
+        perm = np.random.default_rng(1).permutation(a.n_local)
+        b.local[perm] = a.local
+        b.upload()
+        b.table_dev = i32(np.where(a.table >= 0, perm[a.table], -1))
+        q16 = a.queries(400, 4)
+        starts = [0, 350, 400]
+        lam = np.array([0.5, 0.25], np.float32)
+        for maps in (1, 2):
+            x, y = (run_attention(ema, c, q16, starts, torch.float32, maps, lam) for c in (a, b))
+            torch.cuda.synchronize()
+            assert torch.equal(x, y)
+    finally:
+        a.close()
+        b.close()
