@@ -16,7 +16,9 @@
 // weights in LDS, and multiplies all 64 with one of the two V heads: as many products of
 // scores as of V, none done twice. Waves take turns in two groups as in prompt
 // attention, but with two places for tiles: a tile's K, and V of the one before, are sent for
-// at the start of the two phases before those that read it and have arrived at their end.
+// at the start of the two phases before those that read it and have arrived at their end. The
+// group that has its softmax then sends for all of it, so that nothing stands before the
+// other's products (each sending for half: 2.4 us a tile, so: 0.0).
 // Outputs of 32 bits keep the weights in 2 (f16) or 3 (bf16) 16-bit parts, whose place in LDS
 // leaves room for four waves only.
 #include "prompt_common.h"
@@ -212,44 +214,27 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) q[x][ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
   }
-  // m, and 1 / l (the second map's times lambda): each half of the wave joins one map's parts
+  // m, and 1 / l (the second map's times lambda): each half of the wave joins one map's parts,
+  // the first of which are on their way while the first tile is sent for
+  const f32x4* const ml = reinterpret_cast<const f32x4*>(
+      a.ws + (row * a.q_heads + 2 * head + half) * stat_room(stat_splits) * 2);
+  const int n_ml = stat_room(stat_splits) / 2;
+  f32x4 part[4];
+#pragma unroll
+  for (int y = 0; y < 4; ++y) part[y] = ml[min(y, n_ml - 1)];
+  const float factor = half == 0 ? 1.0f : a.lam[head];
   float ref[2], by[2];
-  {
-    const f32x4* ml = reinterpret_cast<const f32x4*>(
-        a.ws + (row * a.q_heads + 2 * head + half) * stat_room(stat_splits) * 2);
-    const int n = stat_room(stat_splits) / 2;
-    float m = -INFINITY, l = 0.0f;
-    for (int y0 = 0; y0 < n; y0 += 8) {
-      f32x4 part[8];
-#pragma unroll
-      for (int y = 0; y < 8; ++y) part[y] = ml[min(y0 + y, n - 1)];
-#pragma unroll
-      for (int y = 0; y < 8; ++y)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (2 * (y0 + y) + e >= stat_splits) continue;
-          const float pm = part[y][2 * e], pl = part[y][2 * e + 1];
-          const float m_new = fmaxf(m, pm), r = m_new == -INFINITY ? 0.0f : m_new;
-          l = l * __builtin_amdgcn_exp2f(m - r) + pl * __builtin_amdgcn_exp2f(pm - r);
-          m = m_new;
-        }
-    }
-    const float mine_ref = m == -INFINITY ? 0.0f : m;
-    const float mine_by = l == 0.0f ? 0.0f : (half == 0 ? 1.0f : a.lam[head]) / l;
-    const float other_ref = other_half(mine_ref), other_by = other_half(mine_by);
-    ref[0] = half == 0 ? mine_ref : other_ref;
-    ref[1] = half == 0 ? other_ref : mine_ref;
-    by[0] = half == 0 ? mine_by : other_by;
-    by[1] = half == 0 ? other_by : mine_by;
-  }
 
   const uint32_t lds_k = lds_address(&s_k[0][0][0]), lds_v = lds_address(&s_v[0][0][0]);
-  Staging<BSC, kThreads> st;
-  typename Staging<BSC, kThreads>::Blocks next_v;
+  constexpr int kSenders = 256;          // threads: the second group, or all
+  const int late = NP == 1 && wave >= kWaves / 2 ? 1 : 0;
+  const bool sends = NP > 1 || late != 0;
+  Staging<BSC, kSenders> st;
+  typename Staging<BSC, kSenders>::Blocks next_v;
   auto place = [&](int j) { return (j - j0) & 1; };
   // K of tile j + 1 and V of tile j are sent for.
   auto send = [&](int j) {
-    if (j >= j1) return;
+    if (j >= j1 || !sends) return;
 #pragma unroll
     for (int x = 0; x < 2; ++x)
       st.load_v(lds_v + (place(j) * 2 + x) * kTileBytes, j, next_v, x);
@@ -262,7 +247,7 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
   };
   // They are there.
   auto receive = [&](int j) {
-    if (j >= j1) return;
+    if (j >= j1 || !sends) return;
     loads_arrived();
     if ((j + 1) * kKT > at.from + 1 || st.window.bad != 0)
 #pragma unroll 1
@@ -375,8 +360,36 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
   if (j0 < j1) {
     st.open(a, R.b, 2 * pair, j0, at.end);
     next_v = st.blocks(j0);
+    if (sends)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) st.load_k(lds_k + x * kTileBytes, j0, next_v, x);
+      for (int x = 0; x < 2; ++x) st.load_k(lds_k + x * kTileBytes, j0, next_v, x);
+  }
+  {
+    float m = -INFINITY, l = 0.0f;
+    for (int y0 = 0; y0 < n_ml; y0 += 4) {
+      if (y0 > 0)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) part[y] = ml[min(y0 + y, n_ml - 1)];
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (2 * (y0 + y) + e >= stat_splits) continue;
+          const float pm = part[y][2 * e], pl = part[y][2 * e + 1];
+          const float m_new = fmaxf(m, pm), r = m_new == -INFINITY ? 0.0f : m_new;
+          l = l * __builtin_amdgcn_exp2f(m - r) + pl * __builtin_amdgcn_exp2f(pm - r);
+          m = m_new;
+        }
+    }
+    const float mine_ref = m == -INFINITY ? 0.0f : m;
+    const float mine_by = l == 0.0f ? 0.0f : factor / l;
+    const float other_ref = other_half(mine_ref), other_by = other_half(mine_by);
+    ref[0] = half == 0 ? mine_ref : other_ref;
+    ref[1] = half == 0 ? other_ref : mine_ref;
+    by[0] = half == 0 ? mine_by : other_by;
+    by[1] = half == 0 ? other_by : mine_by;
+  }
+  if (j0 < j1) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
 #pragma unroll
@@ -387,9 +400,8 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
     loads_arrived();
     __syncthreads();
     // Phase 2j: the first group has the products of tile j, the second weighs tile j - 1;
-    // 2j + 1: the other way round. Both send at the start of 2j and receive at the end of
-    // 2j + 1.
-    const int late = NP == 1 && wave >= kWaves / 2 ? 1 : 0;
+    // 2j + 1: the other way round. Tiles are sent for at the start of 2j and received at the
+    // end of 2j + 1.
     if (late) {
       send(j0);
       __syncthreads();

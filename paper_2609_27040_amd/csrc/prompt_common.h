@@ -400,8 +400,8 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
       (const __attribute__((address_space(3))) void*)p));
 }
 
-// Loads tiles of K and V of a workgroup's sequence into LDS. Place p of a tile is loaded by
-// thread p % THREADS; which piece belongs there is in the offsets. A wave's 64 places of one
+// Loads tiles of K and V of a workgroup's sequence into LDS, by THREADS of its threads. Place p
+// of a tile is loaded by the (p % THREADS)-th of them; which piece belongs there is in the offsets. A wave's 64 places of one
 // round lie in one block, the same for K and V. `head` counts from the workgroup's first KV
 // head: a head's K and V both take 256 * block_size bytes.
 template <int BSC, int THREADS>
@@ -417,9 +417,10 @@ struct Staging {
   uint32_t k_off[kPieces], v_off[kPieces];           // bytes in the block
   IdWindow window;
 
+  static __device__ __forceinline__ int thread() { return int(threadIdx.x) % THREADS; }
   // Of sequence b, whose first `end` tokens (one at least) are looked at, from tile j0 on.
   __device__ __forceinline__ void open(const PromptArgs& a, int b, int kvh, int j0, int end) {
-    const int tid = threadIdx.x;
+    const int tid = thread();
     local = a.local;
     block_bytes = a.block_bytes;
     shift = a.block_shift;
@@ -439,13 +440,13 @@ struct Staging {
   // The channel, the eight tokens of its block and the first token of the tile that piece x of
   // this thread's V is.
   static __device__ __forceinline__ int channel(int x) {
-    return (x * THREADS + int(threadIdx.x)) % kPer / (BSC / 8);
+    return (x * THREADS + thread()) % kPer / (BSC / 8);
   }
   static __device__ __forceinline__ int group(int x) {
-    return (x * THREADS + int(threadIdx.x)) % (BSC / 8) ^ v_turn<BSC>(channel(x));
+    return (x * THREADS + thread()) % (BSC / 8) ^ v_turn<BSC>(channel(x));
   }
   static __device__ __forceinline__ int token(int x) {
-    return (x * THREADS + int(threadIdx.x)) / kPer * BSC + group(x) * 8;
+    return (x * THREADS + thread()) / kPer * BSC + group(x) * 8;
   }
   // Where tile j's pieces are; tiles in ascending order.
   __device__ __forceinline__ Blocks blocks(int j) {
@@ -477,7 +478,7 @@ struct Staging {
   __device__ __forceinline__ void clean_v(u32x4* tile, int j, int end, int* first, int* any) const {
 #pragma unroll
     for (int x = 0; x < kPieces; ++x) {
-      u32x4* at = tile + x * THREADS + threadIdx.x;
+      u32x4* at = tile + x * THREADS + thread();
       u32x4 v = *at;
       const int tok = j * kKT + token(x);
       const int left = window.bad == 0 || window.good(tok >> shift) ? end - tok : 0;
