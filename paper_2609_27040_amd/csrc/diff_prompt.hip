@@ -18,7 +18,7 @@
 // attention, but with two places for tiles: a tile's K, and V of the one before, are sent for
 // at the start of the two phases before those that read it and have arrived at their end. The
 // group that has its softmax then sends for all of it, so that nothing stands before the
-// other's products (each sending for half: 2.4 us a tile, so: 0.0).
+// other's products (each sending for half: three 8B prompts 141 us a call, so: 130).
 // Outputs of 32 bits keep the weights in 2 (f16) or 3 (bf16) 16-bit parts, whose place in LDS
 // leaves room for four waves only.
 #include "prompt_common.h"
@@ -488,8 +488,11 @@ __global__ __launch_bounds__(256) void diff_add(PromptArgs a, int stat_splits, i
 }
 
 // How the two launches are cut: tiles of rows at most, whatever the lengths, and the parts
-// that a tile's tokens are cut into (as many as fill 256 compute units, of 256 tokens at
-// least where the table is full).
+// that a tile's tokens are cut into. A part of the first launch costs a row 8 bytes: it takes
+// what makes 1024 workgroups of them, two of which share a compute unit, but no more than 8
+// unless they are needed to fill the chip. (256 / 512 / 1024 / 2048 workgroups, us a call: three
+// 8B prompts 132 / 132 / 123 / 132, one of 4096 tokens 255 / 256 / 239 / 249; two chunks
+// of 33 and 65 tokens, where 1024 would be 64 parts, 58 / 58 / 64 / 63.)
 struct Cut {
   int64_t stat_tiles, mul_tiles;
   int stat_splits, mul_splits;
@@ -501,14 +504,13 @@ Cut cut_of(const PromptArgs& a) {
   auto tiles = [&](int n) {
     return std::min<int64_t>(a.tokens, (rows + n - 1) / n + a.batch - 1);
   };
-  auto splits = [&](int64_t groups) {
-    return int(std::max<int64_t>(1, std::min<int64_t>({256 / groups, most, 64})));
-  };
   Cut c;
   c.stat_tiles = tiles(kStatRows);
   c.mul_tiles = tiles(mul_rows);
-  c.stat_splits = splits(c.stat_tiles * a.kv_heads);
-  c.mul_splits = splits(c.mul_tiles * (a.kv_heads / 2));
+  const int64_t groups = c.stat_tiles * a.kv_heads;
+  c.stat_splits = int(std::max<int64_t>(
+      1, std::min<int64_t>({1024 / groups, std::max<int64_t>(8, 256 / groups), most, 64})));
+  c.mul_splits = split_parts(a, c.mul_tiles * (a.kv_heads / 2));
   return c;
 }
 

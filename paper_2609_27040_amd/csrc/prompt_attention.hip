@@ -308,13 +308,7 @@ int64_t tile_bound(const PromptArgs& a) {
   return std::min<int64_t>(a.tokens, (rows + kRows - 1) / kRows + a.batch - 1);
 }
 
-// Parts that a tile's tokens are cut into: as many as fill the chip, a workgroup to each of
-// 256 compute units, of 256 tokens at least where the table is full.
-int split_count(const PromptArgs& a) {
-  const int64_t groups = tile_bound(a) * a.kv_heads;
-  const int64_t most = int64_t(a.max_blocks) * a.block_size / 256;
-  return int(std::max<int64_t>(1, std::min<int64_t>({256 / groups, most, 64})));
-}
+int split_count(const PromptArgs& a) { return split_parts(a, tile_bound(a) * a.kv_heads); }
 
 template <bool BF16, int NP>
 hipError_t launch(const PromptArgs& a, hipStream_t stream) {

@@ -5,6 +5,8 @@
 #include "attn_store.h"
 #include "op_kernels.h"
 
+#include <algorithm>
+
 namespace ema {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -14,7 +16,36 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kKT = 64;                 // tokens of a staged tile
+
 constexpr int kTilePieces = kKT * 16;   // 16-byte pieces of a tile's K, and of its V
+
+// Parts that the tokens of a launch's `groups` row tiles are cut into, each of 256 tokens at
+// least where the table is full: the number with the least time by this estimate, in tiles of
+// 1.7 us. A workgroup takes its tiles and some 5 more (it starts and writes its rows); 256 run
+// at once, longest first, and the last, shortest ones leave half of the chip idle; a
+// part's outputs, as many bytes as the rows have in 32 bits, are written and read at 5 TB/s in
+// a further launch. (As many as fit on the chip at once, against this: 2 chunks of some 1250
+// tokens behind 2250, 16 query and 2 KV heads, 157 workgroups, 1 part 112 us, 2 parts 92. Not
+// counting the idle half takes 3 parts for 2 chunks of 200 behind 20000, 64 and 8 heads, where
+// 2 fill the chip: 347 us for 274.)
+inline int split_parts(const PromptArgs& a, int64_t groups) {
+  const double tiles = double(a.max_blocks) * a.block_size / kKT;
+  const double chunk = double(a.tokens) / a.batch / kKT;
+  const double mean = std::max(1.0, tiles - chunk / 2), last = std::max(1.0, tiles - chunk);
+  const double join = 2.0 * a.tokens * a.q_heads * 128 * 4 / 5e6 / 1.7;
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s == 1 || (s <= 64 && s * 4 <= tiles); ++s) {
+    const double work = double(groups) * s / 256 * (mean / s + 5);
+    const double t = std::max(tiles / s + 5, groups * s <= 256 ? 0 : work + (last / s + 5) / 2) +
+                     (s > 1 ? s * join + 2 : 0);
+    if (s == 1 || t < least) {
+      best = s;
+      least = t;
+    }
+  }
+  return best;
+}
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
@@ -138,7 +169,7 @@ __device__ __forceinline__ int wave_max(int x) {
 // a tile's level is how many tiles of rows its last token lies before the longest
 // sequence's end, so a sequence has one tile at most of each level. (Four prompts of
 // 257-3841 tokens, sequence by sequence: 246-270 us by their order, the last tile of each
-// first: 240, so: 000.) Every wave searches alone, 64 sequences at a time.
+// first: 240, so: 215.) Every wave searches alone, 64 sequences at a time.
 constexpr int kLevelBatch = 512;
 template <int ROWS>
 __device__ __forceinline__ RowTile find_by_level(const PromptArgs& a, int group, int index) {
