@@ -151,8 +151,8 @@ int ema_paged_prompt_attention(ema_slice_t h, const void* q, int64_t q_stride,
  * layer is folded into it). out: device [batch][num_q_heads / 2][2 * head_dim] of out_dtype,
  * 16-byte aligned. q as for ema_paged_prompt_attention (row b is sequence b's);
  * block_table, seq_lens, scale as for ema_paged_decode_attention; length 0 gives zeros.
- * num_kv_heads must be even, num_q_heads / num_kv_heads a whole number. Async on
- * `stream`; `workspace` of ema_paged_diff_workspace bytes. Errors: INVAL, HIP.
+ * num_kv_heads must be even, num_q_heads / num_kv_heads a whole number up to 16. Async
+ * on `stream`; `workspace` of ema_paged_diff_workspace bytes. Errors: INVAL, HIP.
  */
 int ema_paged_diff_workspace(ema_slice_t h, int32_t batch, int32_t num_q_heads,
                              int32_t max_blocks, size_t* bytes);
@@ -166,8 +166,8 @@ int ema_paged_diff_attention(ema_slice_t h, const void* q, int64_t q_stride,
 /*
  * paged_diff_prompt_attention -- differential attention of prompt chunks: heads,
  * lambda and norm as for ema_paged_diff_attention, rows, positions and masks as
- * for ema_paged_prompt_attention; out: device
- * [tokens][num_q_heads / 2][2 * head_dim]. `workspace` of
+ * for ema_paged_prompt_attention (any whole number of query heads per KV head); out:
+ * device [tokens][num_q_heads / 2][2 * head_dim]. `workspace` of
  * ema_paged_diff_prompt_workspace bytes. Errors: INVAL, HIP.
  */
 int ema_paged_diff_prompt_workspace(ema_slice_t h, int32_t tokens, int32_t batch,

@@ -156,6 +156,8 @@ int attn_sizes(const AttnCall& c) {
       c.num_q_heads % hkv != 0 || c.num_q_heads > 4096)
     return inval(c.what, "bad tokens, batch, max_blocks or head counts");
   if (c.maps == 2 && hkv % 2 != 0) return inval(c.what, "the KV heads must pair up");
+  if (!c.chunks && c.num_q_heads / hkv > 16)
+    return inval(c.what, "more than 16 query heads per KV head");
   if (c.batch > 65535) return inval(c.what, "batch above 65535");
   if (int64_t(c.tokens) * (c.num_q_heads / hkv) >= (int64_t(1) << 30))
     return inval(c.what, "tokens * query heads per KV head must be below 2^30");

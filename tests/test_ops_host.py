@@ -173,6 +173,16 @@ def test_single_tokens_and_odd_kv_heads(host):
         ema.slice_destroy(odd)
 
 
+def test_single_tokens_take_16_query_heads_per_kv_head(host):
+    ema, h = host
+    table = np.zeros((1, 1), np.int32)
+    ema.paged_diff_attention(h, _Q(1, 32), table, [1], None, None)
+    assert "16" in refused(ema, ema.paged_diff_attention, h, _Q(1, 34), table, [1], None, None)
+    n = ctypes.c_size_t()
+    assert ema._lib.ema_paged_diff_workspace(h, 1, 34, 1, ctypes.byref(n)) == ema.ERR_INVAL
+    ema.paged_diff_prompt_attention(h, _Q(1, 34), [0, 1], table, [1], None, None)
+
+
 def test_sizes_past_the_limits(host):
     ema, h = host
     n = ctypes.c_size_t()
