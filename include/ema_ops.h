@@ -146,6 +146,7 @@ int ema_paged_prompt_attention(ema_slice_t h, const void* q, int64_t q_stride,
  *   o = sum_t (softmax_t(scale * q[2i] . K[2j]_t)
  *              - lambda[i] * softmax_t(scale * q[2i + 1] . K[2j + 1]_t)) V[j]_t
  *   out[b][i] = o, or, with norm_weight, o / sqrt(mean(o^2) + norm_eps) * norm_weight
+ *   (o = 0 stays 0 where norm_eps is 0)
  * for t < seq_lens[b]. lambda: device float [num_q_heads / 2]; norm_weight:
  * device float [2 * head_dim], 16-byte aligned, or NULL (a constant factor of the
  * layer is folded into it). out: device [batch][num_q_heads / 2][2 * head_dim] of out_dtype,

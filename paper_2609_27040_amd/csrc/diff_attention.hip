@@ -73,9 +73,9 @@ __device__ __forceinline__ void write_head(const PromptArgs& a, int b, int head,
     float sq = r[0] * r[0] + r[1] * r[1] + r[2] * r[2] + r[3] * r[3];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sq += __shfl_xor(sq, o);
-    const float inv = 1.0f / sqrtf(sq / float(kCh) + a.norm_eps);
+    const float inv = sq == 0.0f ? 0.0f : 1.0f / sqrtf(sq / float(kCh) + a.norm_eps);
     const f32x4 w = *reinterpret_cast<const f32x4*>(a.norm_weight + 4 * lane);
-    r = l1 == 0.0f ? r : r * inv * w;
+    r = r * inv * w;
   }
   AttnArgs st;
   st.out = a.out;

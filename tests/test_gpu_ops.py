@@ -326,6 +326,38 @@ def test_diff_attention(ema, lens, H, Hq, bs, dtype, out, norm):
         c.close()
 
 
+@pytest.mark.parametrize("single", [True, False])
+def test_a_zero_row_stays_zero_under_the_norm(ema, single):
+    """One token and lambda 1: both maps are 1, their difference 0, and without an
+    epsilon its norm is 0 / 0."""
+    c = SmallCache(ema, [1, 1, 0], 2, 16, "bf16", seed=25)
+    try:
+        B = len(c.lens)
+        q = dev16(c.queries(B, 4), "bf16")
+        lam, w = torch.ones(2, device="cuda"), torch.full((256,), 3.0, device="cuda")
+        out = torch.full((B, 2, 256), 7.0, device="cuda")
+        if single:
+            ema.paged_diff_attention(c.h, q, c.table_dev, c.lens_dev, lam, out, norm_weight=w)
+        else:
+            ema.paged_diff_prompt_attention(c.h, q[:2], i32([0, 1, 2, 2]), c.table_dev, c.lens_dev,
+                                            lam, out[:2], norm_weight=w)
+            assert torch.all(out[2] == 7.0)
+            out = out[:2]
+        assert torch.all(out == 0)
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("maps", [1, 2])
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f16", "f32")])
+def test_many_query_heads_per_kv_head(ema, maps, dtype, out):
+    c = SmallCache(ema, [130, 40], 2, 16, dtype, seed=26)
+    try:
+        check_attention(ema, c, [21, 40], 80, out, maps)
+    finally:
+        c.close()
+
+
 @pytest.mark.parametrize("maps", [1, 2])
 def test_scale_and_output_of_the_other_type(ema, maps):
     c = SmallCache(ema, [70, 40], 2, 16, "f16", seed=20)
