@@ -68,7 +68,7 @@ int must_check(const ema_slice* h, hipStream_t st, const char* what, bool* yes) 
 int tables_sizes(const ema_slice* h, const ema_kv_tables_args* u) {
   const char* what = "kv_tables";
   if (!h || !u) return inval(what, "NULL argument");
-  if (u->layers < 0 || u->layers > 65535 || u->batch < 0 || u->max_blocks < 0 || u->n_ids < 0 ||
+  if (u->layers < 1 || u->layers > 65535 || u->batch < 0 || u->max_blocks < 0 || u->n_ids < 0 ||
       u->n_slots < 0 || u->staging_slots < 0 || u->stage_n < 0 || u->writeback_cap < 0)
     return inval(what, "a size out of range");
   if (int64_t(u->batch) * u->max_blocks * h->shape.block_size >= (int64_t(1) << 31) ||
@@ -159,10 +159,14 @@ int attn_sizes(const AttnCall& c) {
   if (!c.chunks && c.num_q_heads / hkv > 16)
     return inval(c.what, "more than 16 query heads per KV head");
   if (c.batch > 65535) return inval(c.what, "batch above 65535");
-  if (int64_t(c.tokens) * (c.num_q_heads / hkv) >= (int64_t(1) << 30))
-    return inval(c.what, "tokens * query heads per KV head must be below 2^30");
+  if (int64_t(c.tokens) * c.num_q_heads >= (int64_t(1) << 29))
+    return inval(c.what, "tokens * query heads must be below 2^29");
   if (int64_t(c.max_blocks) * c.h->shape.block_size > (int64_t(1) << 30))
     return inval(c.what, "max_blocks too large");
+  // tiles of 32 tokens and a few more per (request, KV pair) are counted in 32 bits
+  const int64_t tiles = int64_t(c.max_blocks) * c.h->shape.block_size / 32 + 8;
+  if (!c.chunks && c.batch * tiles * (hkv / 2) >= (int64_t(1) << 31))
+    return inval(c.what, "batch * max_blocks too large");
   return EMA_OK;
 }
 
@@ -292,15 +296,15 @@ int ema_kv_tables(ema_slice_t h, const ema_kv_tables_args* args, void* workspace
   const char* what = "kv_tables";
   if (int rc = tables_sizes(h, args)) return rc;
   const ema_kv_tables_args& u = *args;
-  const bool blocks = u.layers > 0 && u.batch > 0;
+  const bool blocks = u.batch > 0;
   if (blocks && ((u.n_ids > 0 && !u.block_ids) || !u.seq_lens || !u.new_lens))
     return inval(what, "NULL array");
   if (u.staging_slots > 0 && u.stage_n > 0 && !u.staging_ids) return inval(what, "NULL array");
   if (!h->host_only) {
     if ((blocks && !u.block_table) || !u.query_start ||
-        (u.layers > 0 && u.n_slots > 0 && !u.slot_map))
+        (u.n_slots > 0 && !u.slot_map))
       return inval(what, "NULL output");
-    if (u.staging_slots > 0 && u.layers > 0 &&
+    if (u.staging_slots > 0 &&
         (!u.prefetch_n || !u.writeback_n || (u.stage_n > 0 && (!u.prefetch_src || !u.prefetch_dst)) ||
          (u.writeback_cap > 0 && (!u.writeback_src || !u.writeback_dst))))
       return inval(what, "NULL list");
@@ -313,7 +317,7 @@ int ema_kv_tables(ema_slice_t h, const ema_kv_tables_args* args, void* workspace
   if (int rc = must_check(h, st, what, &check)) return rc;
   if (check && u.batch > 0)
     if (int rc = check_tables(h, args, st)) return rc;
-  if (h->host_only || u.layers == 0) return EMA_OK;
+  if (h->host_only) return EMA_OK;
   const size_t need = tables_bytes(args);
   if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
     return inval(what, "workspace missing, too small or not 16-byte aligned");
@@ -336,7 +340,7 @@ int ema_kv_store(ema_slice_t h, const void* k_new, int64_t k_stride, const void*
                  int64_t v_stride, const int32_t* slot_map, int32_t tokens, void* stream) try {
   const char* what = "kv_store";
   if (!h) return inval(what, "NULL handle");
-  if (tokens < 0) return inval(what, "tokens < 0");
+  if (tokens < 0 || tokens >= 1 << 29) return inval(what, "tokens must be in [0, 2^29)");
   if (tokens == 0) return EMA_OK;
   const int64_t row = int64_t(h->shape.num_kv_heads) * h->shape.head_dim;
   if (!slot_map || (!h->host_only && (!k_new || !v_new))) return inval(what, "NULL array");

@@ -327,7 +327,6 @@ hipError_t launch(const TablesArgs& a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_kv_tables(const TablesArgs& a, hipStream_t stream) {
-  if (a.u.layers == 0) return hipSuccess;
   return table_items(a.u.layers, a.u.batch, a.u.max_blocks) == 4 ? launch<4>(a, stream)
                                                                 : launch<8>(a, stream);
 }

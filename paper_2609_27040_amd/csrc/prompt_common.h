@@ -35,7 +35,8 @@ inline int split_parts(const PromptArgs& a, int64_t groups) {
   const double join = 2.0 * a.tokens * a.q_heads * 128 * 4 / 5e6 / 1.7;
   int best = 1;
   double least = 0.0;
-  for (int s = 1; s == 1 || (s <= 64 && s * 4 <= tiles); ++s) {
+  // (the last bound keeps grids far below 2^32 threads)
+  for (int s = 1; s == 1 || (s <= 64 && s * 4 <= tiles && groups * s <= 1 << 18); ++s) {
     const double work = double(groups) * s / 256 * (mean / s + 5);
     const double t = std::max(tiles / s + 5, groups * s <= 256 ? 0 : work + (last / s + 5) / 2) +
                      (s > 1 ? s * join + 2 : 0);

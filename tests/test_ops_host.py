@@ -192,6 +192,18 @@ def test_sizes_past_the_limits(host):
                                         (1 << 29, 1, 4, 1)):
         assert size(h, tokens, batch, heads, width, ctypes.byref(n)) == ema.ERR_INVAL
     assert size(h, 5, 1, 4, 1, None) == ema.ERR_INVAL
+    diff = ema._lib.ema_paged_diff_prompt_workspace
+    for f in (size, diff):                             # rows of the output: 32 bits
+        assert f(h, 1 << 27, 1, 4, 1, ctypes.byref(n)) == ema.ERR_INVAL
+        assert f(h, (1 << 27) - 1, 1, 4, 1, ctypes.byref(n)) == ema.OK
+    single = ema._lib.ema_paged_diff_workspace         # tiles of all requests: 32 bits
+    assert single(h, 65535, 4, 1 << 17, ctypes.byref(n)) == ema.ERR_INVAL
+    assert single(h, 65535, 4, 1 << 15, ctypes.byref(n)) == ema.OK
+    one = np.zeros(1, np.int32)
+    assert ema._lib.ema_kv_store(h, None, 256, None, 256, one.ctypes.data, 1 << 29,
+                                 None) == ema.ERR_INVAL
+    a = ema.KVTablesArgs(layers=0, batch=1, max_blocks=1)
+    assert ema._lib.ema_kv_tables_workspace(h, ctypes.byref(a), ctypes.byref(n)) == ema.ERR_INVAL
 
 
 def test_the_table_oracle_on_a_case_by_hand():
