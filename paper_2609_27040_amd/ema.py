@@ -437,10 +437,11 @@ def _scratch(nbytes, workspace, stream, device):
         if nbytes == 0:
             return None, None, 0
         import torch
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if stream != _torch().stream():
-            # allocated for the current stream, used on another
-            workspace.record_stream(torch.cuda.ExternalStream(stream))
+        if stream == _torch().stream():
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        else:                             # memory that nothing on another stream still uses
+            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+                workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
     n = workspace.numel() * workspace.element_size()
     if n < nbytes:
         _bad(f"workspace: {n} bytes, {nbytes} needed")

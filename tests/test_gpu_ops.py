@@ -711,3 +711,33 @@ def test_results_do_not_depend_on_placement_or_width(ema):
     finally:
         a.close()
         b.close()
+
+
+@pytest.mark.parametrize("maps", [1, 2])
+def test_a_workspace_of_another_stream_is_no_memory_still_in_use(ema, maps):
+    """A tensor freed while its own stream has yet to read it: a call on another stream must
+    not take its memory."""
+    c = SmallCache(ema, [3000], 2, 16, "bf16", seed=47)
+    try:
+        q = dev16(c.queries(8, 4), "bf16")
+        starts, lam = i32([0, 8]), torch.full((2,), 0.5, device="cuda")
+        size = ema.paged_prompt_workspace if maps == 1 else ema.paged_diff_prompt_workspace
+        n = size(c.h, 8, 1, 4, c.width)
+        assert n > 0
+        out = torch.empty((8, 4 // maps, 128 * maps), device="cuda")
+        side = torch.cuda.Stream()
+        kept = torch.empty(n, dtype=torch.uint8, device="cuda")
+        x = torch.full((n,), 3, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        kept.copy_(x)
+        del x
+        if maps == 1:
+            ema.paged_prompt_attention(c.h, q, starts, c.table_dev, c.lens_dev, out, stream=side)
+        else:
+            ema.paged_diff_prompt_attention(c.h, q, starts, c.table_dev, c.lens_dev, lam, out,
+                                            stream=side)
+        torch.cuda.synchronize()
+        assert torch.all(kept == 3)
+    finally:
+        c.close()
