@@ -44,6 +44,9 @@ class Chunk:
 
     def __init__(self, cache, new_lens, stream=None):
         self.new = np.asarray(new_lens, dtype=np.int64)
+        if self.new.shape != cache.lens.shape or (self.new < 0).any() or \
+                (self.new > cache.lens).any():
+            raise ValueError("new_lens: one per sequence, in [0, length]")
         self.T = int(self.new.sum())
         L, B, width = cache.tables.shape
         nblk = -(-cache.lens // cache.bs)
@@ -61,8 +64,19 @@ class Chunk:
         self.starts = torch.empty(B + 1, **i32)
         new_list = lambda n: tuple(torch.empty(s, **i32) for s in ((L, n), (L, n), (L,)))
         self.prefetch, self.writeback = new_list(cache.stage_n), new_list(max(self.n_writeback))
-        ema.kv_tables(cache.h, _dev(ids), cache.lens_dev, _dev(self.new), self.block_table,
-                      self.slots, self.starts, staging=_dev(cache.staging),
+        args = (_dev(ids), cache.lens_dev, _dev(self.new))
+        staging = _dev(cache.staging)
+        here = torch.cuda.current_stream()
+        if stream is not None:
+            there = torch.cuda.ExternalStream(ema._stream(stream))
+            if there != here:
+                # what is allocated here is written there: behind what used the memory here
+                # before, and not handed out again before it is done
+                there.wait_stream(here)
+                for t in (*args, staging, self.block_table, self.slots, self.starts,
+                          *self.prefetch, *self.writeback):
+                    t.record_stream(there)
+        ema.kv_tables(cache.h, *args, self.block_table, self.slots, self.starts, staging=staging,
                       prefetch=self.prefetch, writeback=self.writeback, stream=stream)
 
 

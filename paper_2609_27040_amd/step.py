@@ -153,7 +153,8 @@ class StepRunner:
 def run_chunk(w, chunk, layer, stream=None):
     """One step of a paged cache that brings a chunk of new tokens (``w.chunk``):
     layer by layer, the slice blocks that hold older tokens are prefetched,
-    ``layer(l)`` gives the layer's (q, k_new, v_new, out), the new K and V are stored,
+    ``layer(l)`` gives the layer's (q, k_new, v_new, out), whose work is on ``stream`` or done
+    (the chunk's tables too), the new K and V are stored,
     attention reads the chunk's rows against everything before them, and the staged copies that
     took tokens go back to the slice. A layer's staging slot is used again
     ``w.staging_slots`` layers later, behind its write-back on the same stream.

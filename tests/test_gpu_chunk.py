@@ -127,3 +127,24 @@ def test_prompts_in_chunks_then_a_decode_step(layout, graph):
         assert ema.slice_device_errors(w.h) == 0
     finally:
         w.close()
+
+
+def test_tables_built_on_another_stream():
+    cfg = synth.TINY.scaled(q_heads=8, kv_heads=2, dtype="bf16")
+    w = Workload(cfg, layers=3, slice_layout=0, staging_slots=2, lens=np.array([90, 33]), frac=0.5)
+    try:
+        here = w.chunk([40, 33])
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        torch.cuda._sleep(20_000_000)
+        there = w.chunk([40, 33], stream=side)
+        torch.cuda.synchronize()
+        for a, b in ((here.block_table, there.block_table), (here.slots, there.slots),
+                     (here.starts, there.starts), *zip(here.prefetch, there.prefetch),
+                     *zip(here.writeback, there.writeback)):
+            assert torch.equal(a, b)
+        for bad in ([40], [91, 1], [-1, 1]):
+            with pytest.raises(ValueError):
+                w.chunk(bad)
+    finally:
+        w.close()
