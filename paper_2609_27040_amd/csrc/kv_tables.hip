@@ -33,6 +33,11 @@ __device__ __forceinline__ int wave_inclusive_sum(int x) {
   return x;
 }
 
+// Set bits of m below the lane.
+__device__ __forceinline__ int bits_below(unsigned long long m) {
+  return __builtin_amdgcn_mbcnt_hi(uint32_t(m >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(m), 0));
+}
+
 // Sums of N values over the workgroup, for every thread. `s` holds N * kWavesOf ints.
 template <int N>
 __device__ __forceinline__ void block_sum(int (&x)[N], int* s) {
@@ -76,7 +81,7 @@ __global__ __launch_bounds__(kTableThreads, 6) void kv_tables_kernel(TablesArgs 
   constexpr int kPer = (kLists + kTableThreads - 1) / kTableThreads;
   __shared__ int s_first[kLists + 2], s_qs[kLists + 2], s_old[kLists + 2];
   __shared__ int s_ids[kChunk];
-  __shared__ int s_red[9 * kWavesOf];
+  __shared__ int s_red[3 * kWavesOf];
   __shared__ int s_wave[3][kWavesOf];
   const ema_kv_tables_args& u = a.u;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -100,18 +105,24 @@ __global__ __launch_bounds__(kTableThreads, 6) void kv_tables_kernel(TablesArgs 
     bool bad;
     if (i0 + i < i1) own[i] = lens_of(a, b0 + i0 + i, &bad);
   }
-  // 0: blocks, 1: new tokens of the requests before the chunk; 2: new tokens of all; of the
-  // layer's slice blocks, prefetches and write-backs, 3-5: those before the chunk, 6-8: all
-  int sum[9] = {};
-  if (!COUNT && staged && a.chunks > 1)
-    for (int c = tid; c < a.chunks; c += kTableThreads) {
+  // of the layer's slice blocks, prefetches and write-backs, 0-2: those before the chunk, 3 and
+  // 4: all prefetches and write-backs; every wave adds them up for itself
+  int list[5] = {};
+  if (!COUNT && staged && a.chunks > 1) {
+    for (int c = lane; c < a.chunks; c += 64) {
 #pragma unroll
       for (int x = 0; x < 3; ++x) {
         const int v = a.counts[(int64_t(layer) * a.chunks + c) * 3 + x];
-        sum[6 + x] += v;
-        if (c < chunk) sum[3 + x] += v;
+        if (c < chunk) list[x] += v;
+        if (x > 0) list[2 + x] += v;
       }
     }
+#pragma unroll
+    for (int x = 0; x < 5; ++x)
+      list[x] = __builtin_amdgcn_readlane(wave_inclusive_sum(list[x]), 63);
+  }
+  // 0: blocks, 1: new tokens of the requests before the chunk; 2: new tokens of all
+  int sum[3] = {};
   for (int b = tid; b < B; b += kTableThreads) {
     bool bad;
     const Lens l = lens_of(a, b, &bad);
@@ -158,7 +169,11 @@ __global__ __launch_bounds__(kTableThreads, 6) void kv_tables_kernel(TablesArgs 
   }
   __syncthreads();
 
-  // the entries: wave w takes ITEMS runs of 64 consecutive ones
+  // the entries: wave w takes ITEMS runs of 64 consecutive ones. Entry x of those from request
+  // b0 on is request x / MB's, at most 4096 requests on: in 32-bit floats with a reciprocal off
+  // by one step the quotient is off by 2^-10 at most, so its whole part by one.
+  const int x0 = e0 - b0 * MB;
+  const float inv_mb = __builtin_amdgcn_rcpf(float(MB));
   int id[ITEMS], rank[ITEMS][3];
   bool is[ITEMS][3];                 // in the slice; to prefetch; to write back
   int n[3] = {0, 0, 0};
@@ -168,7 +183,15 @@ __global__ __launch_bounds__(kTableThreads, 6) void kv_tables_kernel(TablesArgs 
     id[k] = -1;
     bool away = false, older = false, touched = false;
     if (e < e1) {
-      const int b = e / MB, j = e - b * MB, i = b - b0;
+      const int x = x0 + (e - e0);
+      int i = int(float(x) * inv_mb), j = x - i * MB;
+      if (j < 0) {
+        --i;
+        j += MB;
+      } else if (j >= MB) {
+        ++i;
+        j -= MB;
+      }
       const int f = s_first[i] + j;
       if (f < s_first[i + 1]) {
         const int v = f < u.n_ids ? u.block_ids[int64_t(layer) * u.n_ids + f] : -1;
@@ -186,7 +209,7 @@ __global__ __launch_bounds__(kTableThreads, 6) void kv_tables_kernel(TablesArgs 
 #pragma unroll
     for (int c = 0; c < 3; ++c) {
       const unsigned long long m = __ballot(is[k][c]);
-      rank[k][c] = n[c] + __popcll(m & ((1ull << lane) - 1ull));
+      rank[k][c] = n[c] + bits_below(m);
       n[c] += __popcll(m);
     }
   }
@@ -209,13 +232,13 @@ __global__ __launch_bounds__(kTableThreads, 6) void kv_tables_kernel(TablesArgs 
   if (staged) {
     if (a.chunks == 1) {
 #pragma unroll
-      for (int x = 0; x < 3; ++x)
-        for (int w = 0; w < kWavesOf; ++w) sum[6 + x] += s_wave[x][w];
+      for (int x = 1; x < 3; ++x)
+        for (int w = 0; w < kWavesOf; ++w) list[2 + x] += s_wave[x][w];
     }
     int base[3];
 #pragma unroll
     for (int x = 0; x < 3; ++x) {
-      base[x] = sum[3 + x];
+      base[x] = list[x];
       for (int w = 0; w < wave; ++w) base[x] += s_wave[x][w];
     }
     const int64_t pl = int64_t(layer) * u.stage_n, wl = int64_t(layer) * u.writeback_cap;
@@ -252,7 +275,7 @@ __global__ __launch_bounds__(kTableThreads, 6) void kv_tables_kernel(TablesArgs 
         s_ids[e - e0] = entry;
       }
     }
-    const int n_pf = min(sum[7], u.stage_n), n_wb = min(sum[8], u.writeback_cap);
+    const int n_pf = min(list[3], u.stage_n), n_wb = min(list[4], u.writeback_cap);
     if (chunk == 0 && tid == 0) {
       u.prefetch_n[layer] = n_pf;
       u.writeback_n[layer] = n_wb;
@@ -278,13 +301,12 @@ __global__ __launch_bounds__(kTableThreads, 6) void kv_tables_kernel(TablesArgs 
   __syncthreads();
 
   // slots of the new tokens in the chunk's blocks: a contiguous range of them
-  auto token_at = [&](int e) {             // first new token in entry e or later
-    const int b = e / MB, i = b - b0;
-    if (i >= nloc) return s_qs[nloc];
+  auto token_at = [&](int e, int i) {      // first new token in entry e, of request b0 + i, or later
     const int f = s_qs[i + 1] - s_qs[i];
-    return s_qs[i] + clampi((e - b * MB) * BS - s_old[i], 0, f);
+    return s_qs[i] + clampi((e - (b0 + i) * MB) * BS - s_old[i], 0, f);
   };
-  const int t0 = E ? token_at(e0) : 0, t1 = E ? (e1 == E ? s_qs[nloc] : token_at(e1)) : 0;
+  const int t0 = E ? token_at(e0, 0) : 0;
+  const int t1 = E ? (e1 == (b0 + nloc) * MB ? s_qs[nloc] : token_at(e1, nloc - 1)) : 0;
   int32_t* slots = u.slot_map + int64_t(layer) * u.n_slots;
   for (int t = t0 + tid; t < t1; t += kTableThreads) {
     int lo = 0, hi = nloc;                 // s_qs[lo] <= t < s_qs[hi]
