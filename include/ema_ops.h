@@ -61,6 +61,7 @@ extern "C" {
  * layer, slice blocks past stage_n, write-backs past writeback_cap, new tokens
  * past n_slots or in a block that is not local: clamped or left out (-1), and
  * counted. Async on `stream`; `workspace` of ema_kv_tables_workspace bytes.
+ * layers in [1, 65535], batch * max_blocks * block_size below 2^31.
  * Errors: INVAL (sizes, NULL arrays, workspace too small; in checked mode and
  * host-only also any of the violations above), HIP.
  */
@@ -122,7 +123,8 @@ int ema_kv_store(ema_slice_t h, const void* k_new, int64_t k_stride, const void*
  * EMA_F32 keeps the softmax weights in as many 16-bit parts as 32-bit
  * accuracy takes; the 16-bit types use one part, rounded to nearest, whose error is
  * that of the output's own rounding.
- * Any whole number of query heads per KV head. scale <= 0 means
+ * Any whole number of query heads per KV head; tokens * num_q_heads below 2^29,
+ * batch up to 65535. scale <= 0 means
  * 1/sqrt(head_dim). Async on `stream`; `workspace` of
  * ema_paged_prompt_workspace bytes for these sizes (it does not depend on the
  * lengths). Errors: INVAL (in checked mode and host-only also bad starts, lengths or

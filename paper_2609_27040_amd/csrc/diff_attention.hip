@@ -18,8 +18,13 @@
 // 32 KiB of it and each lane's where the lane will read them, so that a whole tile is
 // always on its way without a register held for it: K of the next tile is sent for as
 // soon as the scores are done, V as soon as its product is. At a segment's end the waves merge
-// in the place of V, with the next segment's first K already under way. A segment that is a whole pair is written, a
-// part of one goes to the workspace, and a second launch joins those.
+// in the place of V, with the next segment's first K already under way. A segment that is a
+// whole pair is written, a part of one goes to the workspace, and a second launch joins those.
+//
+// 1024 operations per 1 KiB of K and V: bound by HBM. 64 sequences of 1024-4096 tokens, 8 KV
+// heads, 672 MB: 114 us, 5.9 TB/s. One
+// sequence of 60001 tokens, 61 MB: 27 us, 16 of them this kernel (3.8 TB/s: 14 tiles a
+// workgroup do not hide its start) and 10 the join of 235 parts.
 #include "prompt_common.h"
 
 #include <algorithm>
@@ -31,7 +36,9 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kIt = 32;                  // tokens of a tile
 constexpr int kCh = 256;                 // channels of a pair's values
-// Tiles that a segment costs a workgroup beyond its own.
+// Tiles that a segment costs a workgroup beyond its own: its queries, its first tile's way from
+// HBM, its merge. (2 / 4 / 8 / 16, us: 64 sequences of 1024-4096 tokens 116 / 114 / 117 / 122,
+// 200 of 10-900 tokens 91 / 83 / 83 / 90.)
 constexpr int kSegCost = 4;
 constexpr int kMaxGrid = 256;
 constexpr int kJoinWaves = 16;

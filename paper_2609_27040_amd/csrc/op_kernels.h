@@ -17,7 +17,7 @@ constexpr int kTableThreads = 512;
 // Table entries that a thread takes, and with it a workgroup. Eight where there are enough of
 // them for 512 workgroups and the rows are not too short for a workgroup's list of its
 // requests, else four, so that small tables still spread over the chip. 80 layers of 128
-// requests of up to 504 blocks, us a call with four / eight / sixteen: 66 / 49 / 51.
+// requests of up to 504 blocks, us a call with four / eight: 53 / 45.
 inline int32_t table_items(int64_t layers, int64_t batch, int64_t max_blocks) {
   return max_blocks >= 8 && layers * batch * max_blocks >= 512 * kTableThreads * 8 ? 8 : 4;
 }
