@@ -10,6 +10,8 @@ A plain, slow, obviously correct restatement of what the hot path computes:
   and releases a victim's whole dependency chain (section 4.1).
 * ``attention``: float64 paged decode attention (textbook scaled dot-product
   attention; the paper uses vLLM's attention and gives no formula).
+* ``ops``: tables and slot maps of a step, the store of a chunk, causal and
+  differential attention of chunks, in float64.
 * ``layout``: the byte layout of one layer-block in each pool.
 * ``invariants``: the properties the paper fixes (exactly-once ownership,
   static-dynamic symmetry after reclaim) plus conservation and the logical

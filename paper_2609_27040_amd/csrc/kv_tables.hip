@@ -12,8 +12,8 @@
 // lists' order does not depend on timing.
 //
 // There is no arithmetic to speak of: one request and one layer is latency (9.1 us with the
-// launch: lengths, prefix, ids, stores), 80 layers of 128 requests (65 MB) take 17 + 28 us, of
-// which the instructions of ballots, prefixes and searches are the most (VALU busy 70 % of the
+// launch: lengths, prefix, ids, stores), 80 layers of 128 requests (65 MB) take 15 + 31 us, of
+// which the instructions of ballots, prefixes and searches are the most (VALU busy half of the
 // time; memory 1.4 TB/s). The quotients by a reciprocal and the lists' counts added up without
 // barriers took 51 us to 46.
 #include "op_kernels.h"
