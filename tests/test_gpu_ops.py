@@ -741,3 +741,18 @@ def test_a_workspace_of_another_stream_is_no_memory_still_in_use(ema, maps):
         assert torch.all(kept == 3)
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("maps", [1, 2])
+@pytest.mark.parametrize("lens,new,H,Hq", [
+    ([300, 40], [300, 33], 2, 200),                      # more than 64 tiles of a sequence
+    ([70, 9, 200, 33, 1, 90, 0, 150], [70, 3, 150, 33, 1, 0, 0, 66], 2, 8),
+    ([70, 9, 200, 33, 1, 90, 0, 150, 81], [70, 3, 150, 33, 1, 0, 0, 66, 80], 2, 8),
+])
+def test_tiles_of_few_sequences(ema, maps, lens, new, H, Hq):
+    c = SmallCache(ema, lens, H, 16, "bf16", seed=48)
+    try:
+        check_attention(ema, c, new, Hq, "bf16", maps)
+        assert ema.slice_device_errors(c.h) == 0
+    finally:
+        c.close()
