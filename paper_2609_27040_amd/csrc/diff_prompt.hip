@@ -437,7 +437,8 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
   if (splits > 1) {
     const int64_t rows = int64_t(a.tokens) * (a.q_heads / 2);
     write_rows(scratch, o, 1.0f, out_row, 256, mine * 128,
-               a.ws + int64_t(stat_room(stat_splits)) * a.tokens * a.q_heads * 2 + split * rows * 256, kOutF32);
+               a.ws + int64_t(stat_room(stat_splits)) * a.tokens * a.q_heads * 2 + split * rows * 256,
+               kOutF32);
     return;
   }
   float inv = 1.0f;

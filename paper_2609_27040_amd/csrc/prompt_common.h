@@ -171,7 +171,7 @@ __device__ __forceinline__ int wave_max(int x) {
 // sequence's end, so a sequence has one tile at most of each level. (Four prompts of
 // 257-3841 tokens, sequence by sequence: 246-270 us by their order, the last tile of each
 // first: 240, so: 215.) Every wave searches alone, 64 sequences at a time.
-constexpr int kLevelBatch = 512;
+constexpr int kLevelBatch = 512;         // eight sequences a lane, in registers
 // Sequences up to which a level is found 64 at a time, not by bisection: 4 prompts of 257-3841
 // tokens 210 us (by bisection 216), 16 of 100-500 tokens 49.5 (49.2).
 constexpr int kWideBatch = 8;
@@ -450,8 +450,8 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 }
 
 // Loads tiles of K and V of a workgroup's sequence into LDS, by THREADS of its threads. Place p
-// of a tile is loaded by the (p % THREADS)-th of them; which piece belongs there is in the offsets. A wave's 64 places of one
-// round lie in one block, the same for K and V. `head` counts from the workgroup's first KV
+// of a tile is loaded by the (p % THREADS)-th of them; which piece belongs there is in the
+// offsets. A wave's 64 places of one round lie in one block, the same for K and V. `head` counts from the workgroup's first KV
 // head: a head's K and V both take 256 * block_size bytes.
 template <int BSC, int THREADS>
 struct Staging {
