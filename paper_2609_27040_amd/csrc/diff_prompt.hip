@@ -505,15 +505,11 @@ struct Cut {
   int stat_splits, mul_splits;
 };
 Cut cut_of(const PromptArgs& a) {
-  const int64_t rows = int64_t(a.tokens) * (a.q_heads / a.kv_heads);
   const int64_t most = int64_t(a.max_blocks) * a.block_size / 256;
   const int mul_rows = a.out_dtype == kOutF32 ? kMulRows<2> : kMulRows<1>;
-  auto tiles = [&](int n) {
-    return std::min<int64_t>(a.tokens, (rows + n - 1) / n + a.batch - 1);
-  };
   Cut c;
-  c.stat_tiles = tiles(kStatRows);
-  c.mul_tiles = tiles(mul_rows);
+  c.stat_tiles = tile_bound(a, kStatRows);
+  c.mul_tiles = tile_bound(a, mul_rows);
   const int64_t groups = c.stat_tiles * a.kv_heads;
   c.stat_splits = int(std::max<int64_t>(
       1, std::min<int64_t>({1024 / groups, std::max<int64_t>(8, 256 / groups), most, 64})));

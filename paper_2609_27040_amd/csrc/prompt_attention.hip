@@ -311,17 +311,11 @@ __global__ __launch_bounds__(256) void prompt_join(PromptArgs a, int splits) {
   store_out4(st, row * 128 + d, out_f32x4{O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv});
 }
 
-// Tiles of all sequences at most, whatever their lengths.
-int64_t tile_bound(const PromptArgs& a) {
-  const int64_t rows = int64_t(a.tokens) * (a.q_heads / a.kv_heads);
-  return std::min<int64_t>(a.tokens, (rows + kRows - 1) / kRows + a.batch - 1);
-}
-
-int split_count(const PromptArgs& a) { return split_parts(a, tile_bound(a) * a.kv_heads); }
+int split_count(const PromptArgs& a) { return split_parts(a, tile_bound(a, kRows) * a.kv_heads); }
 
 template <bool BF16, int NP>
 hipError_t launch(const PromptArgs& a, hipStream_t stream) {
-  const int64_t tiles = tile_bound(a);
+  const int64_t tiles = tile_bound(a, kRows);
   const int splits = split_count(a);
   const dim3 grid(unsigned(tiles * a.kv_heads * splits));
   switch (a.block_size) {

@@ -19,6 +19,15 @@ constexpr int kKT = 64;                 // tokens of a staged tile
 
 constexpr int kTilePieces = kKT * 16;   // 16-byte pieces of a tile's K, and of its V
 
+// Tiles of `rows` rows of all sequences at most, whatever their lengths: a sequence of n tokens
+// and G heads a KV head has ceil(n * G / rows) of them, which is neither more than n times those of
+// one token nor, added up, more than all rows' and one for every further sequence.
+inline int64_t tile_bound(const PromptArgs& a, int rows) {
+  const int64_t group = a.q_heads / a.kv_heads;
+  return std::min<int64_t>(a.tokens * ((group + rows - 1) / rows),
+                           (a.tokens * group + rows - 1) / rows + a.batch - 1);
+}
+
 // Parts that the tokens of a launch's `groups` row tiles are cut into, each of 256 tokens at
 // least where the table is full: the number with the least time by this estimate, in tiles of
 // 1.7 us. A workgroup takes its tiles and some 5 more (it starts and writes its rows); 256 run
