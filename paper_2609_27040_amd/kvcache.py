@@ -52,7 +52,7 @@ class Chunk:
         nblk = -(-cache.lens // cache.bs)
         used = np.arange(width)[None, :] < nblk[:, None]
         ids = cache.tables[:, used]                             # (b, j) order
-        away = cache.tables >= cache.n_local
+        away = (cache.tables >= cache.n_local) & used           # not what is allocated ahead
         j = np.arange(width)[None, :]
         old = (cache.lens - self.new)[:, None]
         self.n_prefetch = (away & (j * cache.bs < old)).sum(axis=(1, 2)).tolist()

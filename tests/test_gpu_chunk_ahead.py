@@ -1,0 +1,61 @@
+"""Chunks of prompts in a cache whose blocks are allocated ahead of the tokens, as its
+constructor does: the lists' lengths are those of the blocks that hold tokens."""
+import numpy as np
+import pytest
+import torch
+
+import synth
+from harness import Workload, oracle_mirror
+from ops_harness import dev16
+from oracle import ops as oops
+from paper_2609_27040_amd import ema
+from paper_2609_27040_amd.step import run_chunk
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+@pytest.mark.parametrize("checked", [False, True])
+@pytest.mark.parametrize("full,frac,steps", [
+    ([64], 1.0, ([20], [3], [41])),
+    ([130, 17, 64, 1, 200], 0.5, ([50, 17, 0, 1, 33], [80, 0, 7, 0, 100], [0, 0, 57, 0, 67])),
+])
+def test_blocks_ahead_of_the_tokens(full, frac, steps, checked):
+    cfg = synth.TINY.scaled(q_heads=4, kv_heads=2, dtype="bf16")
+    w = Workload(cfg, layers=3, staging_slots=2, lens=np.array(full), frac=frac, checked=checked)
+    st = oracle_mirror(w)
+    rng = np.random.default_rng(3)
+    try:
+        done = np.zeros(len(full), np.int64)
+        for new in steps:
+            done += new
+            w.lens = done.copy()
+            w.lens_dev.copy_(torch.from_numpy(done.astype(np.int32)))
+            chunk = w.chunk(new)
+            assert chunk.prefetch[2].tolist() == chunk.n_prefetch
+            assert chunk.writeback[2].tolist() == chunk.n_writeback
+            data = [[synth.random_16bit(rng, (chunk.T, h, w.D), "bf16") for h in (4, 2, 2)]
+                    for _ in range(w.L)]
+            dev = [[dev16(x, "bf16") for x in d] for d in data]
+            out = torch.empty((chunk.T, 4, w.D), dtype=torch.bfloat16, device="cuda")
+            run_chunk(w, chunk, lambda l: (*dev[l], out))
+            used = np.arange(w.maxblk)[None, :] < -(-done // w.bs)[:, None]
+            for l in range(w.L):
+                ref = oops.kv_tables([w.tables[l][used]], w.lens, chunk.new, w.maxblk, w.bs,
+                                     w.n_local, chunk.T, w.staging[l % w.staging_slots][None],
+                                     10 ** 4)
+                n, m = int(ref["prefetch"][2][0]), int(ref["writeback"][2][0])
+                st.prefetch(ref["prefetch"][0][0, :n], ref["prefetch"][1][0, :n])
+                oops.kv_store(st.local, *data[l][1:], ref["slots"][0], w.hkv, w.D, w.bs)
+                st.writeback(ref["writeback"][0][0, :m], ref["writeback"][1][0, :m])
+            torch.cuda.synchronize()
+            assert ema.slice_device_errors(w.h) == 0
+            assert np.array_equal(w.local_view.cpu().numpy(), st.local)
+            assert np.array_equal(w.slice_view.cpu().numpy(), st.slice)
+    finally:
+        w.close()
