@@ -5,7 +5,9 @@
 // is rounded: the first launch finds each row's maximum m and sum l for each map (scores
 // only), the second computes the scores again and multiplies
 //   P = 2^(s1 - m1) / l1 - lambda 2^(s2 - m2) / l2,   rounded once,
-// with V, once for both maps. Against running both softmaxes beside each other with an
+// with V, once for both maps. In f16 a row's P is multiplied by a power of two before it is
+// rounded, which the outputs are divided by: P is about 1 / length, where f16's steps of 2^-24
+// show (32-bit outputs, 8191 tokens of scores of deviation 1/4: off by 2e-4 without). Against running both softmaxes beside each other with an
 // output for each, that is the same number of products (scores of 2 x 128 twice, V of 256
 // once, instead of scores once and V twice), half the registers for outputs, no
 // rescaling, and an error of the weights that is relative to the difference.
@@ -196,6 +198,8 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
   __shared__ __attribute__((aligned(16))) u32x4 s_v[2][2][kTilePieces];
   __shared__ __attribute__((aligned(16))) u32x4 s_p[kWaves][2][NP][64];    // a wave's weights
   __shared__ int s_find[kFindScratch];
+  // f16: what a lane's outputs are multiplied by at the end (registers are short)
+  __shared__ float s_back[BF16 ? 1 : kThreads];
   __shared__ int s_bad[2 * 128 + 1];     // the first token not finite, per channel and of all
   float* const s_sq = reinterpret_cast<float*>(&s_p[0][0][0][0]);          // at the end
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -393,6 +397,13 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
     ref[1] = half == 0 ? other_ref : mine_ref;
     by[0] = half == 0 ? mine_by : other_by;
     by[1] = half == 0 ? other_by : mine_by;
+    if constexpr (!BF16) {
+      // 2^(s - m) is at most 2^kSlack, so with the larger factor in [32, 64) P stays below 2^15
+      const int up = 6 - __builtin_amdgcn_frexp_expf(fmaxf(by[0], fabsf(by[1])));
+      by[0] = __builtin_amdgcn_ldexpf(by[0], up);
+      by[1] = __builtin_amdgcn_ldexpf(by[1], up);
+      s_back[tid] = __builtin_amdgcn_ldexpf(1.0f, -up);
+    }
   }
   if (j0 < j1) {
 #pragma unroll
@@ -426,6 +437,11 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
   }
   __syncthreads();
 
+  if constexpr (!BF16) {
+    const float back = s_back[tid];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] *= back;
+  }
   if (s_bad[256] != INT_MAX)
 #pragma unroll
     for (int c = 0; c < 4; ++c)
