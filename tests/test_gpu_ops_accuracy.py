@@ -75,3 +75,15 @@ def error(ema, op, n, rows, out_dtype, sink=0.0):
 def test_differential_chunks_of_many_small_weights(ema, n, rows):
     assert error(ema, "diff-prompt", n, rows, torch.float32) <= 1e-5
     assert error(ema, "diff-prompt", n, rows, torch.float16) <= 2 * 2.0 ** -11
+
+
+# A first token that takes most of the weight and adds nothing, its score 12 above the others: they
+# are off by 2^-25 of a scale in which the largest weight is 2^11 at least, 2.4e-6 of
+# them; its own score of 12 * sqrt(128) before scaling by 8 * 136 * 2^-24 / sqrt(128) = 6e-6,
+# which all of them share. With 5e-6 as above 1.3e-5, and twice that for two maps.
+SINK, SINK_ERR = 12.0, 3e-5
+
+
+@pytest.mark.parametrize("n,rows", [(2048, 5), (8191, 5), (60000, 2)])
+def test_prompts_whose_first_token_takes_the_weight(ema, n, rows):
+    assert error(ema, "prompt", n, rows, torch.float32, SINK) <= SINK_ERR
