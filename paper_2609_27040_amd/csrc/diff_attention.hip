@@ -10,7 +10,9 @@
 // for both maps. At the end o = o1 / l1 - lambda o2 / l2 and, where asked, its norm over
 // the 256 channels. Weights keep NP 16-bit parts, each rounded to nearest (two for
 // 16-bit outputs, since the maps' difference is smaller than the maps; for 32-bit outputs
-// two in f16, 22 bits, and three in bf16, 24).
+// two in f16, 22 bits, and three in bf16, 24). In f16 weights and their sum are 2^15 times as
+// large, so that the smallest step, 2^-24, is 2^-39 of the largest weight (without: a row whose
+// first token has all the weight and no value, 12 above the other scores, was off by 7e-4).
 //
 // Work: 32-token tiles of one (sequence, KV pair), 32 KiB each, all of them in a row
 // cut into equal ranges, one per workgroup, one workgroup to a CU. The four waves of a
@@ -360,11 +362,12 @@ __global__ __launch_bounds__(kThreads, CT == 1 ? 2 : 1) void diff_kernel(PromptA
         const float ref = m_new == -INFINITY ? 0.0f : m_new;
         alpha[ct] = __builtin_amdgcn_exp2f(m[ct] - ref);
         m[ct] = m_new;
+        const float low = BF16 ? ref : ref - 15.0f;
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float x = __builtin_amdgcn_exp2f(sv[2 * i] - ref);
-          float y = __builtin_amdgcn_exp2f(sv[2 * i + 1] - ref);
+          float x = __builtin_amdgcn_exp2f(sv[2 * i] - low);
+          float y = __builtin_amdgcn_exp2f(sv[2 * i + 1] - low);
           sum += x + y;
 #pragma unroll
           for (int r = 0; r < NP; ++r) {
