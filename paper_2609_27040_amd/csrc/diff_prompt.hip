@@ -7,10 +7,13 @@
 //   P = 2^(s1 - m1) / l1 - lambda 2^(s2 - m2) / l2,   rounded once,
 // with V, once for both maps. In f16 a row's P is multiplied by a power of two before it is
 // rounded, which the outputs are divided by: P is about 1 / length, where f16's steps of 2^-24
-// show (32-bit outputs, 8191 tokens of scores of deviation 1/4: off by 2e-4 without). Against running both softmaxes beside each other with an
-// output for each, that is the same number of products (scores of 2 x 128 twice, V of 256
-// once, instead of scores once and V twice), half the registers for outputs, no
-// rescaling, and an error of the weights that is relative to the difference.
+// show (32-bit outputs, 8191 tokens of scores of deviation 1/4: off by 2e-4 without). The
+// maxima are a row's own there, not the last that its sum was scaled by, so the larger map's
+// largest weight stands at 2^13 at least, and the step is 2^-37 of it. Against running both
+// softmaxes beside each other with an output for each, that is the same number of products
+// (scores of 2 x 128 twice, V of 256 once, instead of scores once and V twice), half the
+// registers for outputs, no rescaling, and an error of the weights that is relative to the
+// difference.
 //
 // First launch: as prompt attention without its V half; 256 rows of one KV head to a
 // workgroup. Second: rows are (token, head of the group) of a pair of KV heads, 32 of them
@@ -116,7 +119,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int 
     EMA_SCHED_MFMA(kAhead);
     __builtin_amdgcn_s_setprio(0);
   };
-  float m = -INFINITY, l = 0.0f;
+  float m = -INFINITY, l = 0.0f, top = -INFINITY;      // top: the largest score so far
   auto softmax = [&](int j) {
     const int t0 = j * kKT;
     if (t0 >= at.wave_end) return;
@@ -135,6 +138,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int 
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[tt][i]);
     mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
+    top = fmaxf(top, mx);
     if (__ballot(mx > m + kSlack)) {
       const float m_new = fmaxf(m, mx);
       l *= m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
@@ -179,6 +183,12 @@ __global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int 
       atomicAdd(a.err_count, st.window.bad);
   }
   l += other_half(l);
+  if constexpr (!BF16) {
+    if (top > m) {
+      l *= __builtin_amdgcn_exp2f(m - top);
+      m = top;
+    }
+  }
   if (!at.live || half != 0) return;
   const int64_t row = int64_t(R.row0 + at.tok) * a.q_heads + head;
   reinterpret_cast<float2*>(a.ws)[row * stat_room(splits) + split] = float2{m, l};
@@ -398,8 +408,8 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
     by[0] = half == 0 ? mine_by : other_by;
     by[1] = half == 0 ? other_by : mine_by;
     if constexpr (!BF16) {
-      // 2^(s - m) is at most 2^kSlack, so with the larger factor in [32, 64) P stays below 2^15
-      const int up = 6 - __builtin_amdgcn_frexp_expf(fmaxf(by[0], fabsf(by[1])));
+      // 2^(s - m) is at most 1, so with the larger factor in [2^13, 2^14) P stays below 2^15
+      const int up = 14 - __builtin_amdgcn_frexp_expf(fmaxf(by[0], fabsf(by[1])));
       by[0] = __builtin_amdgcn_ldexpf(by[0], up);
       by[1] = __builtin_amdgcn_ldexpf(by[1], up);
       s_back[tid] = __builtin_amdgcn_ldexpf(1.0f, -up);

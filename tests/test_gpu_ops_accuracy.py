@@ -92,3 +92,8 @@ def test_prompts_whose_first_token_takes_the_weight(ema, n, rows):
 @pytest.mark.parametrize("n", [2048, 8191, 60000])
 def test_single_tokens_whose_first_token_takes_the_weight(ema, n):
     assert error(ema, "diff", n, 1, torch.float32, SINK) <= SINK_ERR
+
+
+@pytest.mark.parametrize("n,rows", [(2048, 5), (8191, 5), (60000, 2)])
+def test_differential_chunks_whose_first_token_takes_the_weight(ema, n, rows):
+    assert error(ema, "diff-prompt", n, rows, torch.float32, SINK) <= SINK_ERR
