@@ -251,9 +251,14 @@ void diff_multiply(PromptArgs a, int stat_splits, int splits) {
   Staging<BSC, kSenders> st;
   typename Staging<BSC, kSenders>::Blocks next_v;
   auto place = [&](int j) { return (j - j0) & 1; };
-  // K of tile j + 1 and V of tile j are sent for.
+  // K of tile j + 1 and V of tile j are sent for. The others follow in the table, to know of
+  // entries that are no block.
   auto send = [&](int j) {
-    if (j >= j1 || !sends) return;
+    if (j >= j1) return;
+    if (!sends) {
+      st.pass(j);
+      return;
+    }
 #pragma unroll
     for (int x = 0; x < 2; ++x)
       st.load_v(lds_v + (place(j) * 2 + x) * kTileBytes, j, next_v, x);

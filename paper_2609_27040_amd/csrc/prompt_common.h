@@ -517,6 +517,8 @@ struct Staging {
                             block_bytes;
     return t;
   }
+  // On to tile j, for a wave that loads none of it.
+  __device__ __forceinline__ void pass(int j) { window.seek(min((j * kKT) >> shift, last)); }
   // `to`: the tile's address in LDS.
   __device__ __forceinline__ void load_k(uint32_t to, int j, const Blocks& t, int head) const {
     const int in = BSC == 64 ? ((j * kKT) & mask) * 256 : 0;   // of block size 128 and more
