@@ -81,6 +81,8 @@ __global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int 
     atomicAdd(a.err_count, 1);
   const Reach at = reach_of<kStatRows>(R, G, R.first + wave * 32, split, splits);
   const int j0 = at.j0, j1 = at.j1, head = query_head(kvh, G, at.g);
+  // the sequence's last rows see all of its tokens
+  const bool counts = kvh == 0 && wave == 0 && R.first + kStatRows >= R.n * G;
 
   u32x4 q[8];
   {
@@ -95,6 +97,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int 
   auto stage = [&](int j, int s2) {
     if (j >= j1) return;
     loads_arrived();
+    if (st.window.bad != 0 && counts) st.count_bad(a, j, at.end);
     if (j + 2 < j1) st.load_k(lds_k + s2 * kTileBytes, j + 2, st.blocks(j + 2), 0);
   };
   f32x16 s[2] = {f32x16{}, f32x16{}};
@@ -179,8 +182,6 @@ __global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int 
       __syncthreads();
     }
     if (!late) __syncthreads();
-    if (st.window.bad != 0 && kvh == 0 && R.first == 0 && tid == 0)
-      atomicAdd(a.err_count, st.window.bad);
   }
   l += other_half(l);
   if constexpr (!BF16) {

@@ -86,6 +86,8 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
     atomicAdd(a.err_count, 1);
   const Reach at = reach_of<kRows>(R, G, R.first + wave * 32, split, splits);
   const int j0 = at.j0, j1 = at.j1;
+  // the sequence's last rows see all of its tokens
+  const bool counts = kvh == 0 && wave == 0 && R.first + kRows >= R.n * G;
 
   u32x4 q[8];
   {
@@ -106,6 +108,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
     loads_arrived();
     if ((j + 1) * kKT > at.from + 1 || st.window.bad != 0)      // some row masks some token
       st.template clean_v<BF16>(s_v[s0], j, at.end, s_bad, &s_bad[128]);
+    if (st.window.bad != 0 && counts) st.count_bad(a, j, at.end);
     if (j + 1 < j1) st.load_v(lds_v + s1 * kTileBytes, j + 1, next_v, 0);
     if (j + 2 < j1) {
       next_v = st.blocks(j + 2);
@@ -258,8 +261,6 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
     }
     products(j1, s2, s0);
     if (!late) __syncthreads();
-    if (st.window.bad != 0 && kvh == 0 && R.first == 0 && tid == 0)
-      atomicAdd(a.err_count, st.window.bad);
   }
   __syncthreads();
 

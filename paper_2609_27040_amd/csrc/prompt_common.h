@@ -519,6 +519,15 @@ struct Staging {
   }
   // On to tile j, for a wave that loads none of it.
   __device__ __forceinline__ void pass(int j) { window.seek(min((j * kKT) >> shift, last)); }
+  // Counts the entries of tile j whose block begins there, before token `end`, and is not of the
+  // pool; one wave of those that see a sequence's tiles does. (window.bad takes whole windows, of
+  // which a part of the tiles holds some only.)
+  __device__ __forceinline__ void count_bad(const PromptArgs& a, int j, int end) const {
+    const int lane = threadIdx.x & 63, tok = j * kKT + lane * 16;
+    const bool bad = lane < kKT / 16 && tok < end && (tok & mask) == 0 && !window.good(tok >> shift);
+    const int n = __popcll(__ballot(bad));
+    if (n > 0 && lane == 0) atomicAdd(a.err_count, n);
+  }
   // `to`: the tile's address in LDS.
   __device__ __forceinline__ void load_k(uint32_t to, int j, const Blocks& t, int head) const {
     const int in = BSC == 64 ? ((j * kKT) & mask) * 256 : 0;   // of block size 128 and more

@@ -75,3 +75,34 @@ def test_a_bad_entry_far_into_the_table(ema, op, out):
             assert np.abs(got[row] - ref).max() < (2.0 ** -8 if out == "bf16" else 1e-4)
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,new,bs", [
+    ([300, 0, 5], [300, 0, 5], 16),                      # several tiles of rows
+    ([4000, 700], [4, 1], 16),                           # the tokens in several parts
+    ([1500, 1000, 129], [40, 1000, 129], 64),
+    ([1025, 2049], [1, 2049], 256),
+])
+@pytest.mark.parametrize("op", ["prompt", "diff-prompt"])
+def test_bad_entries_of_chunks_are_counted_once(ema, op, lens, new, bs, out):
+    c = SmallCache(ema, lens, 4, bs, "bf16", seed=51)
+    try:
+        T = sum(new)
+        q16, starts = c.queries(T, 8), np.concatenate([[0], np.cumsum(new)])
+        maps = 1 if op == "prompt" else 2
+        q, lam = dev16(q16, "bf16"), torch.ones(4, device="cuda")
+        o = torch.zeros((T, 8 // maps, maps * D), dtype=OUT[out], device="cuda")
+        for places in ([(0, 0)], [(0, -1)], [(b, j) for b, n in enumerate(lens)
+                                             for j in range(0, -(-n // bs), 3)]):
+            table = c.table.copy()
+            for b, j in places:
+                table[b, j % max(1, -(-lens[b] // bs))] = -7
+            bad = sum(int((table[b, :-(-n // bs)] == -7).sum()) for b, n in enumerate(lens))
+            if op == "prompt":
+                ema.paged_prompt_attention(c.h, q, i32(starts), i32(table), c.lens_dev, o)
+            else:
+                ema.paged_diff_prompt_attention(c.h, q, i32(starts), i32(table), c.lens_dev, lam, o)
+            assert ema.slice_device_errors(c.h) == bad
+    finally:
+        c.close()
