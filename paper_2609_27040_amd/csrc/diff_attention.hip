@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kThreads, CT == 1 ? 2 : 1) void diff_kernel(PromptA
     const char* at[2];
     int ok;                              // bit h: the half's block is of the pool
   };
-  auto locate = [&](IdWindow& w, int j) {
+  auto locate = [&](IdWindow& w, const Segment& g, int j) {
     Place p;
     const int t0 = j * kIt;
     w.seek(min(t0 >> a.block_shift, w.last));
@@ -219,9 +219,16 @@ __global__ __launch_bounds__(kThreads, CT == 1 ? 2 : 1) void diff_kernel(PromptA
       p.at[h] = a.local + int64_t(w.get(min((t0 >> a.block_shift) + h, w.last))) * Bb;
     }
     p.ok = 3;
-    if (w.bad != 0)
-      p.ok = (w.good(t0 >> a.block_shift) ? 1 : 0) |
-             (w.good((t0 + 16) >> a.block_shift) ? 2 : 0);
+    if (w.bad != 0) {
+      p.ok = 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int tok = t0 + 16 * h;
+        if (w.good(tok >> a.block_shift)) p.ok |= 1 << h;
+        else if (g.pair == 0 && lane == 0 && tok < g.len && (tok & (BS - 1)) == 0)
+          atomicAdd(a.err_count, 1);     // the tile that the block begins in
+      }
+    }
     return p;
   };
   // K rows: subtile t, row r16 -> token t0 + 8 * (r16 / 4) + 4t + r16 % 4 (every lane ends
@@ -296,7 +303,7 @@ __global__ __launch_bounds__(kThreads, CT == 1 ? 2 : 1) void diff_kernel(PromptA
   auto open = [&](const Segment& s) {
     if (s.j0 + wave >= s.j1) return;
     win.open(a, s.b, ((s.j0 + wave) * kIt) >> a.block_shift, (s.len - 1) >> a.block_shift);
-    at = locate(win, s.j0 + wave);
+    at = locate(win, s, s.j0 + wave);
     load_k(s, at, s.j0 + wave);
   };
   auto open_v = [&](const Segment& s) {
@@ -341,7 +348,7 @@ __global__ __launch_bounds__(kThreads, CT == 1 ? 2 : 1) void diff_kernel(PromptA
       }
       reads_done();
       if (more) {
-        at = locate(win, j + kWaves);
+        at = locate(win, g, j + kWaves);
         load_k(g, at, j + kWaves);
       }
       const int n = g.len - j * kIt - 8 * q4;        // valid tokens of this lane's 8
@@ -416,8 +423,6 @@ __global__ __launch_bounds__(kThreads, CT == 1 ? 2 : 1) void diff_kernel(PromptA
       for (int c = 0; c < 16; ++c)
         part_at(wave, colx, 4 * c + q4) = o[ct][c];
     }
-    if (win.bad != 0 && g.pair == 0 && tid == 0)
-      atomicAdd(a.err_count, win.bad);
     const Segment done = g;
     have = next_segment(g);
     if (have) {

@@ -106,3 +106,25 @@ def test_bad_entries_of_chunks_are_counted_once(ema, op, lens, new, bs, out):
             assert ema.slice_device_errors(c.h) == bad
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("heads", [2, 9])
+@pytest.mark.parametrize("lens,bs", [([2100, 777, 40, 0], 16), ([1057], 16), ([900, 33] * 9, 32),
+                                     ([1500, 64], 64), ([30] * 300, 16), ([600, 255], 256)])
+def test_bad_entries_of_single_tokens_are_counted_once(ema, lens, bs, heads):
+    c = SmallCache(ema, lens, 4, bs, "bf16", seed=52)
+    try:
+        B = len(lens)
+        q, lam = dev16(c.queries(B, 4 * heads), "bf16"), torch.ones(2 * heads, device="cuda")
+        o = torch.zeros((B, 2 * heads, 2 * D), device="cuda")
+        for step in (1, 3, 64):
+            table = c.table.copy()
+            table[:, ::step] = c.n_local
+            table[:, -1] = -9                            # behind every length: not looked at
+            bad = sum(len(range(0, -(-n // bs), step)) for n in lens)
+            ema.paged_diff_attention(c.h, q, i32(table), c.lens_dev, lam, o)
+            assert ema.slice_device_errors(c.h) == bad
+            if step == 1:
+                assert (o == 0).all()
+    finally:
+        c.close()
