@@ -76,6 +76,7 @@ __global__ __launch_bounds__(kStatThreads, 2) void diff_stats(PromptArgs a, int 
   const int kvh = int(blockIdx.x) % a.kv_heads, rest = int(blockIdx.x) / a.kv_heads;
   const int split = rest % splits;
   const RowTile R = find_tile<kStatThreads, kStatRows>(a, G, rest / splits, s_find);
+  if (blockIdx.x == 0 && R.wrong > 0) atomicAdd(a.err_count, R.wrong);
   if (R.b < 0) return;
   if (R.first == 0 && split == 0 && kvh == 0 && tid == 0 && (R.len < R.n || R.len != R.given))
     atomicAdd(a.err_count, 1);

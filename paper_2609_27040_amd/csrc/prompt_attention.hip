@@ -81,6 +81,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a, int s
   const int split = rest % splits;
   if (tid < 129) s_bad[tid] = INT_MAX;
   const RowTile R = find_tile<kThreads, kRows>(a, G, rest / splits, s_find);
+  if (blockIdx.x == 0 && R.wrong > 0) atomicAdd(a.err_count, R.wrong);
   if (R.b < 0) return;
   if (R.first == 0 && split == 0 && kvh == 0 && tid == 0 && (R.len < R.n || R.len != R.given))
     atomicAdd(a.err_count, 1);

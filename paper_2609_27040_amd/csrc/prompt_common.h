@@ -147,12 +147,15 @@ struct RowTile {
   int first;      // first (token, head) pair of the tile
   int len;        // tokens of the sequence
   int given;      // its length as it is given
+  int wrong;      // of the sequences this thread looked at: those whose rows are no range of q's
 };
 
-// Rows of sequence b in q, clamped to what is there.
-__device__ __forceinline__ void row_range(const PromptArgs& a, int b, int& s, int& n) {
-  s = min(max(a.starts[b], 0), a.tokens);
-  n = max(0, min(a.starts[b + 1], a.tokens) - s);
+// Rows of sequence b in q, clamped to what is there; 1 if the starts are out of range.
+__device__ __forceinline__ int row_range(const PromptArgs& a, int b, int& s, int& n) {
+  const int from = a.starts[b], to = a.starts[b + 1];
+  s = min(max(from, 0), a.tokens);
+  n = max(0, min(to, a.tokens) - s);
+  return from < 0 || to < from || to > a.tokens || (b == 0 && from != 0);
 }
 
 // Sum and maximum (of values >= 0) over the wave's 64 lanes, uniform: DPP moves within
@@ -190,20 +193,22 @@ __device__ __forceinline__ RowTile find_by_level(const PromptArgs& a, int group,
   const int lane = threadIdx.x & 63;
   int tiles[N], start[N], rows[N], len[N], skip[N];   // of sequences 64 * i + lane
   int total = 0, longest = 0;
+  RowTile r;
+  r.wrong = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     tiles[i] = rows[i] = start[i] = len[i] = 0;
     if (i * 64 >= a.batch) continue;
     const int b = i * 64 + lane;
     if (b < a.batch) {
-      row_range(a, b, start[i], rows[i]);
+      r.wrong += row_range(a, b, start[i], rows[i]);
       len[i] = a.seq_lens[b];
     }
     tiles[i] = (rows[i] * group + ROWS - 1) / ROWS;
     total += tiles[i];
     if (tiles[i] > 0) longest = max(longest, len[i]);
   }
-  RowTile r;
+  if (threadIdx.x >= 64) r.wrong = 0;    // every wave looks at all sequences
   r.b = -1;
   if (index >= wave_sum(total)) return r;
   longest = wave_max(longest);
@@ -282,9 +287,11 @@ __device__ __forceinline__ RowTile find_in_order(const PromptArgs& a, int group,
   const int per = (a.batch + THREADS - 1) / THREADS;
   const int b0 = min(a.batch, tid * per), b1 = min(a.batch, b0 + per);
   int total = 0;
+  RowTile r;
+  r.wrong = 0;
   for (int b = b0; b < b1; ++b) {
     int s, n;
-    row_range(a, b, s, n);
+    r.wrong += row_range(a, b, s, n);
     total += (n * group + ROWS - 1) / ROWS;
   }
   int incl = total;
@@ -315,7 +322,6 @@ __device__ __forceinline__ RowTile find_in_order(const PromptArgs& a, int group,
     }
   }
   __syncthreads();
-  RowTile r;
   r.b = uniform(out[0]);
   if (r.b < 0) return r;
   r.row0 = uniform(out[1]);

@@ -128,3 +128,40 @@ def test_bad_entries_of_single_tokens_are_counted_once(ema, lens, bs, heads):
                 assert (o == 0).all()
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("starts,bad", [([1, 3, 10], 1), ([0, 6, 2], 1), ([0, 12, 11], 2),
+                                        ([-4, 3, 10], 1), ([0, 3, 2 ** 31 - 1], 1)])
+@pytest.mark.parametrize("maps", [1, 2])
+def test_bad_starts_are_counted(ema, maps, starts, bad):
+    """Starts that do not begin at 0, descend or pass the rows: a request each."""
+    c = SmallCache(ema, [64, 40], 2, 16, "bf16", seed=53)
+    try:
+        q, lam = dev16(c.queries(10, 4), "bf16"), torch.ones(2, device="cuda")
+        o = torch.zeros((10, 4 // maps, maps * D), device="cuda")
+        if maps == 1:
+            ema.paged_prompt_attention(c.h, q, i32(starts), c.table_dev, c.lens_dev, o)
+        else:
+            ema.paged_diff_prompt_attention(c.h, q, i32(starts), c.table_dev, c.lens_dev, lam, o)
+        assert ema.slice_device_errors(c.h) == bad
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("B", [100, 700])
+@pytest.mark.parametrize("maps", [1, 2])
+def test_bad_starts_among_many_requests_are_counted(ema, maps, B):
+    c = SmallCache(ema, [3] * B, 2, 16, "bf16", seed=57)
+    try:
+        q, lam = dev16(c.queries(B, 4), "bf16"), torch.ones(2, device="cuda")
+        o = torch.zeros((B, 4 // maps, maps * D), device="cuda")
+        starts = np.arange(B + 1)
+        starts[[70, 71]] = starts[[71, 70]]              # request 70 ends before it begins
+        starts[B] = B + 5                                # the last one ends past the rows
+        if maps == 1:
+            ema.paged_prompt_attention(c.h, q, i32(starts), c.table_dev, c.lens_dev, o)
+        else:
+            ema.paged_diff_prompt_attention(c.h, q, i32(starts), c.table_dev, c.lens_dev, lam, o)
+        assert ema.slice_device_errors(c.h) == 2
+    finally:
+        c.close()
