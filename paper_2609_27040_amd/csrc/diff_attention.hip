@@ -1,11 +1,10 @@
 // Differential attention of one token per sequence over the paged cache, on the
 // matrix cores.
 //
-// The two maps of the G heads that share a pair of KV heads are columns of one
-// product: with the pair's keys side by side (256 channels), map 1 of head g is a
-// query that is zero past channel 128, map 2 one that is zero before it, so one tile of
-// scores S^T[token][map, head] = K1 . [Q1 | 0] + K2 . [0 | Q2] holds both (G <= 8: one
-// 16-wide tile; above, a tile for each map). Softmax runs per column as in plain
+// The two maps of the G heads that share a pair of KV heads are columns of one tile of
+// scores S^T[token][map, head], with both maps' queries side by side as the B operand: the
+// columns of map 1 are taken from K1 . [Q1 | Q2], those of map 2 from K2 . [Q1 | Q2]
+// (G <= 8: one 16-wide tile; above, a tile for each map). Softmax runs per column as in plain
 // decode; O^T[channel][map, head] += [V1 V2]^T . P^T has 256 channels and reads V once
 // for both maps. At the end o = o1 / l1 - lambda o2 / l2 and, where asked, its norm over
 // the 256 channels. Weights keep NP 16-bit parts, each rounded to nearest (two for
@@ -328,14 +327,15 @@ __global__ __launch_bounds__(kThreads, CT == 1 ? 2 : 1) void diff_kernel(PromptA
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         if constexpr (CT == 1) {
-          const bool first = r16 < 8;
-          const u32x4 none = {0, 0, 0, 0};
-          s[0][t] = f32x4{};
+          // each map's keys by all columns, of which the other map's are not looked at: with
+          // zeros there for a query an infinite key would reach them as NaN
+          f32x4 x = f32x4{}, y = f32x4{};
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
-            s[0][t] = mfma16<BF16>(k[0][t][kk], first ? q[0][kk] : none, s[0][t]);
-            s[0][t] = mfma16<BF16>(k[1][t][kk], first ? none : q[0][kk], s[0][t]);
+            x = mfma16<BF16>(k[0][t][kk], q[0][kk], x);
+            y = mfma16<BF16>(k[1][t][kk], q[0][kk], y);
           }
+          s[0][t] = r16 < 8 ? x : y;
         } else {
 #pragma unroll
           for (int ct = 0; ct < 2; ++ct) {
