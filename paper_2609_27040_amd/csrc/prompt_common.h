@@ -440,17 +440,17 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, uint
   const uint64_t ub = uint64_t(uint32_t(uniform(int(uint32_t(b))))) |
                       uint64_t(uint32_t(uniform(int(uint32_t(b >> 32))))) << 32;
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :: "s"(uniform(int(lds))), "v"(off), "s"(ub) : "memory");
+               :: "s"(uniform(int(lds))), "v"(off), "s"(ub) : "memory", "m0");
 }
 // The same from an address per lane; NT: streamed past the caches.
 template <bool NT>
 __device__ __forceinline__ void load_lane_to_lds(const char* p, uint32_t lds) {
   if constexpr (NT)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt"
-                 :: "s"(uniform(int(lds))), "v"(p) : "memory");
+                 :: "s"(uniform(int(lds))), "v"(p) : "memory", "m0");
   else
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                 :: "s"(uniform(int(lds))), "v"(p) : "memory");
+                 :: "s"(uniform(int(lds))), "v"(p) : "memory", "m0");
 }
 // All of the wave's loads but the newest 16 have arrived.
 __device__ __forceinline__ void loads_arrived_but_16() {
