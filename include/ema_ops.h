@@ -28,6 +28,8 @@
 extern "C" {
 #endif
 
+#define EMA_FULL_WEIGHTS 0x100   /* with an out_dtype: softmax weights of 32-bit accuracy */
+
 /*
  * kv_tables -- the tables of a step for all layers, from the requests' lengths
  * (section 4: a request's logical blocks map to segments of the slice or to
@@ -121,8 +123,11 @@ int ema_kv_store(ema_slice_t h, const void* k_new, int64_t k_stride, const void*
  * what a row's mask leaves out may hold anything, infinities and NaN too.
  * out: device [tokens][num_q_heads][head_dim] of out_dtype, 16-byte aligned.
  * EMA_F32 keeps the softmax weights in as many 16-bit parts as 32-bit
- * accuracy takes; the 16-bit types use one part, rounded to nearest, whose error is
- * that of the output's own rounding.
+ * accuracy takes (f16 two, in a power-of-two scale that keeps them from f16's
+ * smallest steps; bf16 three); the 16-bit types use one part, rounded to nearest,
+ * whose error is that of the output's own rounding (together 1.3 to 1.6 times it).
+ * EMA_F16 and EMA_BF16 may be given with EMA_FULL_WEIGHTS: as EMA_F32, in its
+ * time, and rounded once at the end.
  * Any whole number of query heads per KV head; tokens * num_q_heads below 2^29,
  * batch up to 65535. scale <= 0 means
  * 1/sqrt(head_dim). Async on `stream`; `workspace` of
@@ -154,6 +159,7 @@ int ema_paged_prompt_attention(ema_slice_t h, const void* q, int64_t q_stride,
  * layer is folded into it). out: device [batch][num_q_heads / 2][2 * head_dim] of out_dtype,
  * 16-byte aligned. q as for ema_paged_prompt_attention (row b is sequence b's);
  * block_table, seq_lens, scale as for ema_paged_decode_attention; length 0 gives zeros.
+ * The 16-bit types use weights in two parts here (bf16: 16 bits), EMA_FULL_WEIGHTS as above.
  * num_kv_heads must be even, num_q_heads / num_kv_heads a whole number up to 16. Async
  * on `stream`; `workspace` of ema_paged_diff_workspace bytes. Errors: INVAL, HIP.
  */

@@ -577,7 +577,7 @@ void launch_sizes(const PromptArgs& a, int grid, hipStream_t stream) {
 template <int CT>
 void launch_types(const PromptArgs& a, int grid, hipStream_t stream) {
   if (a.dtype == 0) launch_sizes<CT, false, 2>(a, grid, stream);
-  else if (a.out_dtype == kOutF32) launch_sizes<CT, true, 3>(a, grid, stream);
+  else if (a.full) launch_sizes<CT, true, 3>(a, grid, stream);
   else launch_sizes<CT, true, 2>(a, grid, stream);
 }
 

@@ -539,7 +539,7 @@ struct Cut {
 };
 Cut cut_of(const PromptArgs& a) {
   const int64_t most = int64_t(a.max_blocks) * a.block_size / 256;
-  const int mul_rows = a.out_dtype == kOutF32 ? kMulRows<2> : kMulRows<1>;
+  const int mul_rows = a.full ? kMulRows<2> : kMulRows<1>;
   Cut c;
   c.stat_tiles = tile_bound(a, kStatRows);
   c.mul_tiles = tile_bound(a, mul_rows);
@@ -573,11 +573,11 @@ hipError_t launch_sizes(const PromptArgs& a, const Cut& c, hipStream_t stream) {
 }  // namespace
 
 size_t diff_prompt_workspace(const PromptArgs& a) {
-  // the output's type is not known here: the larger of the two cuts
+  // how the weights are kept is not known here: the larger of the two cuts
   PromptArgs b = a;
   size_t most = 0;
-  for (int out : {kOutF32, kOutBF16}) {
-    b.out_dtype = out;
+  for (int full : {0, 1}) {
+    b.full = full;
     const Cut c = cut_of(b);
     size_t n = size_t(stat_room(c.stat_splits)) * a.tokens * a.q_heads * 2;
     if (c.mul_splits > 1) n += size_t(c.mul_splits) * a.tokens * (a.q_heads / 2) * 256;
@@ -589,7 +589,7 @@ size_t diff_prompt_workspace(const PromptArgs& a) {
 hipError_t launch_diff_prompt_attention(const PromptArgs& a, hipStream_t stream) {
   const Cut c = cut_of(a);
   hipError_t e;
-  if (a.out_dtype != kOutF32)
+  if (!a.full)
     e = a.dtype == 1 ? launch_sizes<true, 1>(a, c, stream) : launch_sizes<false, 1>(a, c, stream);
   else
     e = a.dtype == 1 ? launch_sizes<true, 3>(a, c, stream) : launch_sizes<false, 2>(a, c, stream);

@@ -197,7 +197,8 @@ ema::PromptArgs kernel_args(const AttnCall& c) {
   a.max_blocks = c.max_blocks;
   a.block_shift = log2_of(a.block_size);
   a.dtype = h->shape.dtype;
-  a.out_dtype = c.out_dtype;
+  a.out_dtype = c.out_dtype & ~EMA_FULL_WEIGHTS;
+  a.full = c.out_dtype == EMA_F32 || (c.out_dtype & EMA_FULL_WEIGHTS) != 0;
   return a;
 }
 
@@ -244,7 +245,8 @@ int check_attention(const AttnCall& c, hipStream_t st) {
 int attention(const AttnCall& c) {
   if (int rc = attn_sizes(c)) return rc;
   const ema_slice* h = c.h;
-  if (c.out_dtype != EMA_F32 && c.out_dtype != EMA_F16 && c.out_dtype != EMA_BF16)
+  const int32_t type = c.out_dtype & ~EMA_FULL_WEIGHTS;
+  if (type != EMA_F32 && type != EMA_F16 && type != EMA_BF16)
     return inval(c.what, "out_dtype must be EMA_F32, EMA_F16 or EMA_BF16");
   if (!(c.norm_eps >= 0.0f)) return inval(c.what, "norm_eps must not be negative");
   if (c.tokens > 0 && c.batch > 0) {

@@ -72,6 +72,7 @@ struct PromptArgs {
   int32_t block_shift;         // log2(block_size)
   int32_t dtype;               // 0 f16, 1 bf16
   int32_t out_dtype;           // kOutF32, kOutF16 or kOutBF16
+  int32_t full;                // softmax weights of 32-bit accuracy
 };
 size_t prompt_workspace(const PromptArgs& a);
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t stream);

@@ -352,7 +352,7 @@ size_t prompt_workspace(const PromptArgs& a) {
 }
 
 hipError_t launch_prompt_attention(const PromptArgs& a, hipStream_t stream) {
-  if (a.out_dtype != kOutF32)
+  if (!a.full)
     return a.dtype == 1 ? launch<true, 1>(a, stream) : launch<false, 1>(a, stream);
   return a.dtype == 1 ? launch<true, 3>(a, stream) : launch<false, 2>(a, stream);
 }

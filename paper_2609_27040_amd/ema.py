@@ -19,6 +19,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "libe
 
 OK, ERR_INVAL, ERR_NOMEM, ERR_OWNER, ERR_HIP = 0, -1, -2, -3, -4
 F16, BF16, F32 = 0, 1, 2
+FULL_WEIGHTS = 0x100
 LAYOUT_ATTN, LAYOUT_NHD = 0, 1
 ENGINE_KERNEL, ENGINE_DMA = 0, 1
 SLAB_LAYER_MAJOR, SLAB_SLAB_MAJOR, SLAB_GROUP_MAJOR = 0, 1, 2
@@ -559,7 +560,7 @@ def kv_store(h, k_new, v_new, slot_map, stream=None):
 
 
 def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out, scale, lam,
-                  norm_weight, norm_eps, workspace, stream):
+                  norm_weight, norm_eps, full_weights, workspace, stream):
     T = _torch()
     rows, Hq = q.shape[0], q.shape[1]
     if len(block_table.shape) != 2:
@@ -588,6 +589,8 @@ def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out,
                  None if norm_weight is None else _dev(norm_weight, "norm_weight", T.f32, 256),
                  float(norm_eps))
     dst = _dev(out, "out", T.out_types, rows * Hq * 128)
+    if full_weights:
+        code |= FULL_WEIGHTS
     st = _stream(stream)
     n = ctypes.c_size_t()
     _check(size(h, *sizes, ctypes.byref(n)))
@@ -616,33 +619,37 @@ def paged_diff_prompt_workspace(h, tokens, batch, num_q_heads, max_blocks):
 
 
 def paged_prompt_attention(h, q, query_start, block_table, seq_lens, out, scale=0.0,
-                           workspace=None, stream=None):
+                           workspace=None, stream=None, full_weights=False):
     """Causal attention of prompt chunks: q [T][Hq][128] (16-bit, tokens any multiple
     of 8 elements apart), query_start int32 [B + 1], block_table int32
     [B][max_blocks], seq_lens int32 [B], out [T][Hq][128] of float32, float16 or
-    bfloat16. Without ``workspace`` (a byte tensor of paged_prompt_workspace bytes)
-    the call takes one from torch's allocator."""
+    bfloat16. A 16-bit out rounds the softmax weights once, or with ``full_weights`` keeps
+    them to 32-bit accuracy as a float32 out does, in its time. Without ``workspace`` (a byte
+    tensor of paged_prompt_workspace bytes) the call takes one from torch's allocator."""
     _attention_op(h, _lib.ema_paged_prompt_attention, _lib.ema_paged_prompt_workspace, 1, q,
-                  query_start, block_table, seq_lens, out, scale, None, None, 0.0, workspace,
-                  stream)
+                  query_start, block_table, seq_lens, out, scale, None, None, 0.0, full_weights,
+                  workspace, stream)
 
 
 def paged_diff_attention(h, q, block_table, seq_lens, lam, out, scale=0.0, norm_weight=None,
-                         norm_eps=0.0, workspace=None, stream=None):
+                         norm_eps=0.0, workspace=None, stream=None, full_weights=False):
     """Differential attention of one token per sequence: q [B][Hq][128], lam float32
     [Hq / 2], out [B][Hq / 2][256]; with norm_weight (float32 [256]) each output
-    row is divided by its root mean square and multiplied by it."""
+    row is divided by its root mean square and multiplied by it. full_weights as in
+    paged_prompt_attention (without it a bfloat16 out has weights of 16 bits)."""
     _attention_op(h, _lib.ema_paged_diff_attention, _lib.ema_paged_diff_workspace, 2, q, None,
-                  block_table, seq_lens, out, scale, lam, norm_weight, norm_eps, workspace, stream)
+                  block_table, seq_lens, out, scale, lam, norm_weight, norm_eps, full_weights,
+                  workspace, stream)
 
 
 def paged_diff_prompt_attention(h, q, query_start, block_table, seq_lens, lam, out, scale=0.0,
-                                norm_weight=None, norm_eps=0.0, workspace=None, stream=None):
+                                norm_weight=None, norm_eps=0.0, workspace=None, stream=None,
+                                full_weights=False):
     """Differential attention of prompt chunks: rows as in paged_prompt_attention,
     heads, lam and norm as in paged_diff_attention; out [T][Hq / 2][256]."""
     _attention_op(h, _lib.ema_paged_diff_prompt_attention, _lib.ema_paged_diff_prompt_workspace, 2,
                   q, query_start, block_table, seq_lens, out, scale, lam, norm_weight, norm_eps,
-                  workspace, stream)
+                  full_weights, workspace, stream)
 
 
 # ---- slab management of the slice --------------------------------------------------

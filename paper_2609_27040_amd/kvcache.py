@@ -225,9 +225,9 @@ class PagedKVCache:
         """The chunk's K and V [T][Hkv][D] into layer l's blocks."""
         ema.kv_store(self.h, k_new, v_new, chunk.slots[l], stream=stream)
 
-    def prompt_attention(self, l, chunk, q, out, stream=None):
+    def prompt_attention(self, l, chunk, q, out, stream=None, full_weights=False):
         ema.paged_prompt_attention(self.h, q, chunk.starts, chunk.block_table[l], self.lens_dev,
-                                   out, stream=stream)
+                                   out, full_weights=full_weights, stream=stream)
 
     def diff_prompt_attention(self, l, chunk, q, lam, out, stream=None, **norm):
         ema.paged_diff_prompt_attention(self.h, q, chunk.starts, chunk.block_table[l],
