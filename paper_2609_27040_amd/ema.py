@@ -462,8 +462,11 @@ def _i32_exact(t, name, host, shape):
 
 def _tables_args(host, block_ids, seq_lens, new_lens, block_table, slot_map, query_start,
                  canon_table, staging, prefetch, writeback):
-    L, B, max_blocks = block_table.shape
-    n_ids, n_slots = block_ids.shape[-1], slot_map.shape[-1]
+    try:
+        L, B, max_blocks = block_table.shape
+        (_, n_ids), (_, n_slots) = block_ids.shape, slot_map.shape
+    except ValueError:
+        _bad("expected block_table [L][B][max_blocks], block_ids [L][n_ids], slot_map [L][n_slots]")
     addr = [_i32_exact(block_ids, "block_ids", host, (L, n_ids)),
             _i32_exact(seq_lens, "seq_lens", host, (B,)),
             _i32_exact(new_lens, "new_lens", host, (B,)), None,
@@ -476,8 +479,13 @@ def _tables_args(host, block_ids, seq_lens, new_lens, block_table, slot_map, que
     if staging is not None:
         if prefetch is None or writeback is None:
             _bad("staging needs the prefetch and writeback lists")
-        slots, stage_n = staging.shape
-        cap = writeback[0].shape[-1]
+        try:
+            slots, stage_n = staging.shape
+            _, _, _ = prefetch
+            to_write, _, _ = writeback
+            _, cap = to_write.shape
+        except ValueError:
+            _bad("expected staging [slots][stage_n] and lists (source [L][n], destination, count)")
         addr[3] = _i32_exact(staging, "staging", host, (slots, stage_n))
         for kind, (src, dst, count), n in (("prefetch", prefetch, stage_n),
                                            ("writeback", writeback, cap)):
@@ -562,10 +570,11 @@ def kv_store(h, k_new, v_new, slot_map, stream=None):
 def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out, scale, lam,
                   norm_weight, norm_eps, full_weights, workspace, stream):
     T = _torch()
-    rows, Hq = q.shape[0], q.shape[1]
-    if len(block_table.shape) != 2:
-        _bad("block_table: expected [batch][max_blocks]")
-    B, max_blocks = block_table.shape
+    try:
+        rows, Hq, _ = q.shape
+        B, max_blocks = block_table.shape
+    except ValueError:
+        _bad("expected q [tokens][heads][128] and block_table [batch][max_blocks]")
     extra = () if maps == 1 else (None, None, float(norm_eps))
     sizes = (rows, B, Hq, max_blocks) if query_start is not None else (B, Hq, max_blocks)
     if query_start is None and rows != B:
