@@ -9,7 +9,8 @@
  * handle takes host arrays, validates them and launches nothing; on a
  * handle made with EMA_CREATE_CHECKED the device arrays are read back and
  * validated first (not while `stream` is capturing: INVAL). Otherwise kernels
- * skip what is out of range and count it (ema_slice_device_errors).
+ * skip what is out of range and count it (ema_slice_device_errors): a table entry,
+ * a length, a request's starts each once a call, however many heads look at them.
  *
  * Workspaces belong to the caller: a call that needs one says how many bytes
  * (ema_*_workspace; 0: none, NULL will do), 16-byte aligned device memory that
@@ -119,8 +120,16 @@ int ema_kv_store(ema_slice_t h, const void* k_new, int64_t k_stride, const void*
  * multiple of 8 and at least num_q_heads * head_dim. query_start: device int32
  * [batch + 1], ascending from 0 to at most `tokens`; rows of out past its last
  * entry stay as they were. A row at a negative position (more queries than
- * tokens) gives zeros and is counted. What lies behind a request's length and
- * what a row's mask leaves out may hold anything, infinities and NaN too.
+ * tokens) gives zeros, and its request is counted. Starts that do not begin at 0,
+ * descend or pass `tokens` are clamped and their requests counted; rows that then
+ * belong to no request, or to two, may stay as they were. What lies behind a request's length and
+ * what a row's mask leaves out may hold anything, infinities and NaN too. A row
+ * that attends an infinity or NaN in V gets something not finite in its channel
+ * (NaN, or the infinity), one that attends NaN in K, or a score of +infinity, NaN.
+ * The tokens are cut into parts by the sizes, types and max_blocks, not by the
+ * lengths: the same call gives the same bits, one with a wider table may differ in
+ * the last ones (and take longer: a table much wider than the lengths makes parts
+ * without tokens).
  * out: device [tokens][num_q_heads][head_dim] of out_dtype, 16-byte aligned.
  * EMA_F32 keeps the softmax weights in as many 16-bit parts as 32-bit
  * accuracy takes (f16 two, in a power-of-two scale that keeps them from f16's
@@ -159,6 +168,7 @@ int ema_paged_prompt_attention(ema_slice_t h, const void* q, int64_t q_stride,
  * layer is folded into it). out: device [batch][num_q_heads / 2][2 * head_dim] of out_dtype,
  * 16-byte aligned. q as for ema_paged_prompt_attention (row b is sequence b's);
  * block_table, seq_lens, scale as for ema_paged_decode_attention; length 0 gives zeros.
+ * Tokens and values that are not finite, and bits and table widths, as above.
  * The 16-bit types use weights in two parts here (bf16: 16 bits), EMA_FULL_WEIGHTS as above.
  * num_kv_heads must be even, num_q_heads / num_kv_heads a whole number up to 16. Async
  * on `stream`; `workspace` of ema_paged_diff_workspace bytes. Errors: INVAL, HIP.
