@@ -73,11 +73,23 @@ class Chunk:
                 # what is allocated here is written there: behind what used the memory here
                 # before, and not handed out again before it is done
                 there.wait_stream(here)
-                for t in (*args, staging, self.block_table, self.slots, self.starts,
-                          *self.prefetch, *self.writeback):
+                for t in (*args, staging):
                     t.record_stream(there)
+        self._users = {here.cuda_stream}
+        self.used_on(stream)
         ema.kv_tables(cache.h, *args, self.block_table, self.slots, self.starts, staging=staging,
                       prefetch=self.prefetch, writeback=self.writeback, stream=stream)
+
+    def used_on(self, stream):
+        """Keeps the tables' memory from being handed out again, once the chunk is gone, before
+        the work queued on ``stream`` is done. The cache's calls do this."""
+        raw = ema._stream(stream)
+        if raw in self._users:
+            return
+        self._users.add(raw)
+        there = torch.cuda.ExternalStream(raw)
+        for t in (self.block_table, self.slots, self.starts, *self.prefetch, *self.writeback):
+            t.record_stream(there)
 
 
 class PagedKVCache:
@@ -218,18 +230,22 @@ class PagedKVCache:
         return Chunk(self, new_lens, stream)
 
     def prefetch_chunk(self, l, chunk, stream=None):
+        chunk.used_on(stream)
         ema.slice_prefetch(self.h, chunk.prefetch[0][l], chunk.prefetch[1][l],
                            chunk.n_prefetch[l], stream=stream)
 
     def store(self, l, chunk, k_new, v_new, stream=None):
         """The chunk's K and V [T][Hkv][D] into layer l's blocks."""
+        chunk.used_on(stream)
         ema.kv_store(self.h, k_new, v_new, chunk.slots[l], stream=stream)
 
     def prompt_attention(self, l, chunk, q, out, stream=None, full_weights=False):
+        chunk.used_on(stream)
         ema.paged_prompt_attention(self.h, q, chunk.starts, chunk.block_table[l], self.lens_dev,
                                    out, full_weights=full_weights, stream=stream)
 
     def diff_prompt_attention(self, l, chunk, q, lam, out, stream=None, **norm):
+        chunk.used_on(stream)
         ema.paged_diff_prompt_attention(self.h, q, chunk.starts, chunk.block_table[l],
                                         self.lens_dev, lam, out, stream=stream, **norm)
 
@@ -241,6 +257,7 @@ class PagedKVCache:
 
     def writeback_chunk(self, l, chunk, stream=None):
         """The staged copies that took the chunk's tokens, back to the slice."""
+        chunk.used_on(stream)
         ema.slice_writeback(self.h, chunk.writeback[0][l], chunk.writeback[1][l],
                             chunk.n_writeback[l], stream=stream)
 

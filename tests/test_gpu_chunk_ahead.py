@@ -59,3 +59,34 @@ def test_blocks_ahead_of_the_tokens(full, frac, steps, checked):
             assert np.array_equal(w.slice_view.cpu().numpy(), st.slice)
     finally:
         w.close()
+
+
+def test_a_chunk_dropped_while_another_stream_uses_it():
+    """The tables' memory is not handed out again before the step on its stream is done."""
+    cfg = synth.TINY.scaled(q_heads=4, kv_heads=2, dtype="bf16")
+    w = Workload(cfg, layers=3, staging_slots=2, lens=np.array([130, 64, 200]), frac=0.5)
+    rng = np.random.default_rng(4)
+    try:
+        new = [130, 64, 200]
+        data = [[dev16(synth.random_16bit(rng, (394, h, w.D), "bf16"), "bf16") for h in (4, 2, 2)]
+                for _ in range(w.L)]
+        outs = [[torch.zeros((394, 4, w.D), dtype=torch.bfloat16, device="cuda")
+                 for _ in range(w.L)] for _ in range(2)]
+        run_chunk(w, w.chunk(new), lambda l: (*data[l], outs[0][l]))
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        chunk = w.chunk(new)
+        sizes = [t.shape for t in (chunk.block_table, chunk.slots, chunk.starts, *chunk.prefetch,
+                                   *chunk.writeback)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(50_000_000)
+        run_chunk(w, chunk, lambda l: (*data[l], outs[1][l]), stream=side)
+        del chunk
+        junk = [torch.full(s, -5, dtype=torch.int32, device="cuda") for s in sizes * 3]
+        torch.cuda.synchronize()
+        assert ema.slice_device_errors(w.h) == 0
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+        del junk
+    finally:
+        w.close()
