@@ -121,11 +121,12 @@ int ema_kv_store(ema_slice_t h, const void* k_new, int64_t k_stride, const void*
  * [batch + 1], ascending from 0 to at most `tokens`; rows of out past its last
  * entry stay as they were. A row at a negative position (more queries than
  * tokens) gives zeros, and its request is counted. Starts that do not begin at 0,
- * descend or pass `tokens` are clamped and their requests counted; rows that then
- * belong to no request, or to two, may stay as they were. What lies behind a request's length and
- * what a row's mask leaves out may hold anything, infinities and NaN too. A row
- * that attends an infinity or NaN in V gets something not finite in its channel
- * (NaN, or the infinity), one that attends NaN in K, or a score of +infinity, NaN.
+ * descend or pass `tokens` are clamped and their requests counted; what rows hold
+ * that then belong to no request, or to two, is not defined. What lies behind a
+ * request's length and what a row's mask leaves out may hold anything, infinities
+ * and NaN too. A row that attends an infinity or NaN in V gets something not
+ * finite in its channel (NaN, or the infinity), one that attends NaN in K, or a
+ * score of +infinity, NaN; one whose scores are all -infinity gives zeros.
  * The tokens are cut into parts by the sizes, types and max_blocks, not by the
  * lengths: the same call gives the same bits, one with a wider table may differ in
  * the last ones (and take longer: a table much wider than the lengths makes parts
