@@ -1,17 +1,15 @@
 """Relative 2-norm errors of attention over long float16 caches, where many small
 weights make up a row.
 
-What they may be. A score is 128 products of exact 16-bit values added up in 32 bits: 8 steps
-of the matrix cores, each off by at most 2^-24 of what is there. With queries of deviation 1/4
-what is there stays below 12 before scaling (8 standard deviations of 1.5 hold
-16 of 128 channels), so a score is off by 8 * 12 * 2^-24 = 5.7e-6, scaled by 1/sqrt(128) 5e-7;
-the exponent's argument, below 32 in the log2 domain, by a few 2^-24 * 32 = 2e-6 * ln 2 each
-way. 5e-6 a weight covers them and the exponential's own 2^-23. Two 16-bit parts keep a weight to 2^-22, or to
-2^-25 in the float16 scale of the row, whose largest weight stands at 32 at least: a weight w
-times smaller than it is off by 2^-30 * w. Errors of different tokens multiply
-independent values, so the row's norm is off by no more than its weights are, and twice as
-much where two maps are subtracted with a factor of 1/2 (|w1| + |w2| / 2 against
-|w1 - w2 / 2| is up to 3 token by token, less in the norm).
+What they may be. A score is 128 products of exact 16-bit values added up in 32 bits, in 8 steps of
+the matrix cores that are each off by at most 2^-24 of the sum so far. With queries of
+deviation 1/4 a sum has deviation 1/4 * sqrt(128) = 2.8 and stays below 16, so a score is off by
+8 * 16 * 2^-24 = 7.6e-6, scaled by 1 / sqrt(128) 7e-7. The exponent's argument, below 32 in the
+log2 domain, is rounded to 2^-24 * 32 = 2e-6, times ln 2 1.3e-6, and so is the maximum taken
+from it; the exponential is off by 2^-23. 5e-6 a weight covers all of them. Two 16-bit parts
+keep a weight to 2^-22 of it. Errors of different tokens multiply independent values, so a row's
+norm is off by no more than its weights are, and twice as much where two maps are subtracted,
+the second with a factor of 1/2: 1e-5.
 A 16-bit output is off by half a step, 2^-11, and so is each of its weights."""
 import numpy as np
 import pytest
