@@ -252,6 +252,15 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def torch_stream(stream, device=None):
+    """The torch stream of what an entry point takes as one."""
+    import torch
+    raw = _stream(stream)
+    # (an ExternalStream of 0 would be one from torch's pool)
+    return torch.cuda.ExternalStream(raw, device=device) if raw else \
+        torch.cuda.default_stream(device)
+
+
 # ---- entry points ---------------------------------------------------------------
 
 def slice_create(num_kv_heads, head_dim, block_size, dtype, slice_layout, local_bytes,
@@ -441,7 +450,7 @@ def _scratch(nbytes, workspace, stream, device):
         if stream == _torch().stream():
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
         else:                             # memory that nothing on another stream still uses
-            with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+            with torch.cuda.stream(torch_stream(stream, device)):
                 workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
     n = workspace.numel() * workspace.element_size()
     if n < nbytes:

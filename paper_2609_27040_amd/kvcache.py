@@ -68,7 +68,7 @@ class Chunk:
         staging = _dev(cache.staging)
         here = torch.cuda.current_stream()
         if stream is not None:
-            there = torch.cuda.ExternalStream(ema._stream(stream))
+            there = ema.torch_stream(stream)
             if there != here:
                 # what is allocated here is written there: behind what used the memory here
                 # before, and not handed out again before it is done
@@ -87,7 +87,7 @@ class Chunk:
         if raw in self._users:
             return
         self._users.add(raw)
-        there = torch.cuda.ExternalStream(raw)
+        there = ema.torch_stream(raw)
         for t in (self.block_table, self.slots, self.starts, *self.prefetch, *self.writeback):
             t.record_stream(there)
 
