@@ -154,7 +154,7 @@ struct RowTile {
 __device__ __forceinline__ int row_range(const PromptArgs& a, int b, int& s, int& n) {
   const int from = a.starts[b], to = a.starts[b + 1];
   s = min(max(from, 0), a.tokens);
-  n = max(0, min(to, a.tokens) - s);
+  n = max(0, min(max(to, 0), a.tokens) - s);
   return from < 0 || to < from || to > a.tokens || (b == 0 && from != 0);
 }
 
