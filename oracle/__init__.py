@@ -12,6 +12,7 @@ A plain, slow, obviously correct restatement of what the hot path computes:
   attention; the paper uses vLLM's attention and gives no formula).
 * ``ops``: tables and slot maps of a step, the store of a chunk, causal and
   differential attention of chunks, in float64.
+* ``trees``: masks, attention, accepted paths and compaction of drafted trees.
 * ``layout``: the byte layout of one layer-block in each pool.
 * ``invariants``: the properties the paper fixes (exactly-once ownership,
   static-dynamic symmetry after reclaim) plus conservation and the logical

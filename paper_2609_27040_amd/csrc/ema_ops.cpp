@@ -1,67 +1,27 @@
-// Entry points of the operators declared in include/ema_ops.h: argument checks,
-// then one launcher each.
+// Entry points of the operators declared in include/ema_ops.h, and of the attention of
+// include/ema_tree.h: argument checks, then one launcher each.
 #include "ema_ops.h"
 
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
-#include <string>
 #include <vector>
 
+#include "op_checks.h"
 #include "op_kernels.h"
 #include "slice_handle.h"
+#include "tree_kernels.h"
 
+using ema::aligned16;
 using ema::DeviceScope;
-using ema::fetch_ints;
+using ema::HostInts;
 using ema::internal_error;
-using ema::set_error;
+using ema::inval;
+using ema::log2_of;
+using ema::must_check;
 
 namespace {
-
-int inval(const char* what, const char* why) {
-  return set_error(EMA_ERR_INVAL, std::string(what) + ": " + why);
-}
-
-int32_t log2_of(int32_t x) {   // of a power of two
-  int32_t s = 0;
-  while ((1 << s) < x) ++s;
-  return s;
-}
-
-bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-
-// The host's view of a device array in checked mode, or the caller's own array on
-// a host-only handle.
-class HostInts {
- public:
-  int get(const ema_slice* h, const int32_t* p, int64_t n, hipStream_t st) {
-    if (h->host_only) {
-      data_ = p;
-      return EMA_OK;
-    }
-    const int rc = fetch_ints(p, n, st, &copy_);
-    data_ = copy_.data();
-    return rc;
-  }
-  int32_t operator[](int64_t i) const { return data_[i]; }
-
- private:
-  const int32_t* data_ = nullptr;
-  std::vector<int32_t> copy_;
-};
-
-// Whether the call's arrays are to be validated on the host; a stream that
-// captures cannot be read back from.
-int must_check(const ema_slice* h, hipStream_t st, const char* what, bool* yes) {
-  *yes = h->host_only || h->checked;
-  if (h->host_only || !h->checked) return EMA_OK;
-  bool capturing = false;
-  if (int rc = ema::is_capturing(st, &capturing)) return rc;
-  return capturing ? inval(what, "a checked handle cannot read its arrays back during stream "
-                                 "capture")
-                   : EMA_OK;
-}
 
 // ---- tables ---------------------------------------------------------------------
 
@@ -147,6 +107,9 @@ struct AttnCall {
   void* workspace;
   size_t workspace_bytes;
   void* stream;
+  bool tree = false;             // mask given
+  const uint64_t* mask = nullptr;
+  int32_t mask_words = 0;
 };
 
 int attn_sizes(const AttnCall& c) {
@@ -205,6 +168,7 @@ ema::PromptArgs kernel_args(const AttnCall& c) {
 size_t attn_bytes(const AttnCall& c) {
   if (c.h->host_only || c.tokens == 0 || c.batch == 0) return 0;
   const ema::PromptArgs a = kernel_args(c);
+  if (c.tree) return ema::tree_workspace(a);
   return c.maps == 1 ? ema::prompt_workspace(a)
                      : (c.chunks ? ema::diff_prompt_workspace(a) : ema::diff_workspace(a));
 }
@@ -249,6 +213,8 @@ int attention(const AttnCall& c) {
   if (type != EMA_F32 && type != EMA_F16 && type != EMA_BF16)
     return inval(c.what, "out_dtype must be EMA_F32, EMA_F16 or EMA_BF16");
   if (!(c.norm_eps >= 0.0f)) return inval(c.what, "norm_eps must not be negative");
+  if (c.tree && (c.mask_words < 1 || c.mask_words > EMA_TREE_WORDS))
+    return inval(c.what, "mask_words must be in [1, EMA_TREE_WORDS]");
   if (c.tokens > 0 && c.batch > 0) {
     if ((!h->host_only && (!c.q || !c.out)) || !c.block_table || !c.seq_lens ||
         (c.chunks && !c.query_start) || (c.maps == 2 && !h->host_only && !c.lambda))
@@ -257,6 +223,8 @@ int attention(const AttnCall& c) {
       return inval(c.what, "q_stride must be a multiple of 8 that holds a token's heads");
     if (!h->host_only && (!aligned16(c.q) || !aligned16(c.out) || !aligned16(c.norm_weight)))
       return inval(c.what, "q, out and norm_weight must be 16-byte aligned");
+    if (c.tree && !h->host_only && (!c.mask || reinterpret_cast<uintptr_t>(c.mask) % 8 != 0))
+      return inval(c.what, "mask missing or not 8-byte aligned");
   }
   if (c.tokens == 0 || c.batch == 0) return EMA_OK;
   if (!h->host_only && h->book.n_local() == 0) return inval(c.what, "the local pool is empty");
@@ -273,6 +241,14 @@ int attention(const AttnCall& c) {
   if (need > 0 && (!c.workspace || c.workspace_bytes < need || !aligned16(c.workspace)))
     return inval(c.what, "workspace missing, too small or not 16-byte aligned");
   const ema::PromptArgs a = kernel_args(c);
+  if (c.tree) {
+    ema::TreeAttnArgs t{};
+    static_cast<ema::PromptArgs&>(t) = a;
+    t.mask = c.mask;
+    t.words = c.mask_words;
+    HIP_TRY(ema::launch_tree_attention(t, st), c.what);
+    return EMA_OK;
+  }
   HIP_TRY(c.maps == 1 ? ema::launch_prompt_attention(a, st)
                       : (c.chunks ? ema::launch_diff_prompt_attention(a, st)
                                   : ema::launch_diff_attention(a, st)),
@@ -473,6 +449,36 @@ int ema_paged_diff_prompt_attention(ema_slice_t h, const void* q, int64_t q_stri
   return attention({"diff_prompt_attention", 2, true, h, q, q_stride, query_start, block_table,
                     seq_lens, tokens, batch, num_q_heads, max_blocks, scale, lambda, norm_weight,
                     norm_eps, out, out_dtype, workspace, workspace_bytes, stream});
+} catch (...) {
+  return internal_error();
+}
+
+int ema_paged_tree_workspace(ema_slice_t h, int32_t tokens, int32_t batch, int32_t num_q_heads,
+                             int32_t max_blocks, size_t* bytes) try {
+  AttnCall c{};
+  c.what = "tree_attention";
+  c.maps = 1;
+  c.chunks = true;
+  c.tree = true;
+  c.h = h;
+  c.tokens = tokens;
+  c.batch = batch;
+  c.num_q_heads = num_q_heads;
+  c.max_blocks = max_blocks;
+  return workspace_call(c, bytes);
+} catch (...) {
+  return internal_error();
+}
+
+int ema_paged_tree_attention(ema_slice_t h, const void* q, int64_t q_stride,
+                             const int32_t* query_start, const int32_t* block_table,
+                             const int32_t* seq_lens, const uint64_t* mask, int32_t mask_words,
+                             int32_t tokens, int32_t batch, int32_t num_q_heads,
+                             int32_t max_blocks, float scale, void* out, int32_t out_dtype,
+                             void* workspace, size_t workspace_bytes, void* stream) try {
+  return attention({"tree_attention", 1, true, h, q, q_stride, query_start, block_table, seq_lens,
+                    tokens, batch, num_q_heads, max_blocks, scale, nullptr, nullptr, 0.0f, out,
+                    out_dtype, workspace, workspace_bytes, stream, true, mask, mask_words});
 } catch (...) {
   return internal_error();
 }

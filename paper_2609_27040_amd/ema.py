@@ -126,6 +126,12 @@ def _load():
         "ema_paged_diff_prompt_workspace": [P, I32, I32, I32, I32, PSZ],
         "ema_paged_diff_prompt_attention": [P, P, I64, P, P, P, I32, I32, I32, I32, F32C, P, P,
                                             F32C, P, I32, P, SZ, P],
+        "ema_tree_tables": [P, P, P, P, I32, I32, P, I32, P, P, P],
+        "ema_paged_tree_workspace": [P, I32, I32, I32, I32, PSZ],
+        "ema_paged_tree_attention": [P, P, I64, P, P, P, P, I32, I32, I32, I32, I32, F32C, P, I32,
+                                     P, SZ, P],
+        "ema_tree_accept": [P, P, P, P, P, P, I32, I32, I32, P, P, P, P],
+        "ema_kv_compact": [P, P, P, P, P, I32, I32, I32, I32, P, P],
         "ema_sched_create": [I32, I32, I64, ctypes.POINTER(P)],
         "ema_sched_destroy": [P],
         "ema_sched_place": [P, I32, I32, I32, I64, P, ctypes.POINTER(I32)],
@@ -167,6 +173,7 @@ class _Torch:
         self.out_types = tuple(self.out_codes)
         self.i32 = (torch.int32,)
         self.f32 = (torch.float32,)
+        self.i64 = (torch.int64,)
         self.kv16 = {F16: (torch.float16,), BF16: (torch.bfloat16,)}
         self.any16 = (torch.float16, torch.bfloat16, torch.int16)
         raw, dev = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream",
@@ -577,7 +584,7 @@ def kv_store(h, k_new, v_new, slot_map, stream=None):
 
 
 def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out, scale, lam,
-                  norm_weight, norm_eps, full_weights, workspace, stream):
+                  norm_weight, norm_eps, full_weights, workspace, stream, mask=None):
     T = _torch()
     try:
         rows, Hq, _ = q.shape
@@ -592,7 +599,8 @@ def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out,
     if rec[0] if rec else _host_only(h):
         table, lens = _i32_host(block_table), _i32_host(seq_lens)
         starts = () if query_start is None else (_i32_host(query_start).ctypes.data,)
-        _check(fn(h, None, Hq * 128, *starts, table.ctypes.data, lens.ctypes.data, *sizes,
+        masks = () if mask is None else (None, mask.shape[1])
+        _check(fn(h, None, Hq * 128, *starts, table.ctypes.data, lens.ctypes.data, *masks, *sizes,
                   float(scale), *extra, None, F32, None, 0, None))
         return
     code = T.out_codes.get(out.dtype)
@@ -602,6 +610,7 @@ def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out,
     starts = () if query_start is None else (_i32_dev(query_start, "query_start", B + 1),)
     table = _i32_dev(block_table, "block_table", B * max_blocks)
     lens = _i32_dev(seq_lens, "seq_lens", B)
+    masks = () if mask is None else _mask_words(mask, rows)
     if maps == 2:
         extra = (_dev(lam, "lam", T.f32, Hq // 2),
                  None if norm_weight is None else _dev(norm_weight, "norm_weight", T.f32, 256),
@@ -613,8 +622,8 @@ def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out,
     n = ctypes.c_size_t()
     _check(size(h, *sizes, ctypes.byref(n)))
     ws, p, nbytes = _scratch(n.value, workspace, st, q.device)
-    _check(fn(h, qp, qs, *starts, table, lens, *sizes, float(scale), *extra, dst, code, p, nbytes,
-              st))
+    _check(fn(h, qp, qs, *starts, table, lens, *masks, *sizes, float(scale), *extra, dst, code, p,
+              nbytes, st))
 
 
 def _size_call(fn, *args):
@@ -668,6 +677,121 @@ def paged_diff_prompt_attention(h, q, query_start, block_table, seq_lens, lam, o
     _attention_op(h, _lib.ema_paged_diff_prompt_attention, _lib.ema_paged_diff_prompt_workspace, 2,
                   q, query_start, block_table, seq_lens, out, scale, lam, norm_weight, norm_eps,
                   full_weights, workspace, stream)
+
+
+# ---- trees of drafted tokens (include/ema_tree.h) -------------------------------------
+
+def _i32_args(host, arrays):
+    """Addresses of int32 arrays (name, array or None, elements it must have)."""
+    T = _torch() if not host else None
+    addr = []
+    for name, t, n in arrays:
+        if t is None:
+            addr.append(None)
+        elif host:
+            if not isinstance(t, np.ndarray) or t.dtype != np.int32 or not t.flags.c_contiguous:
+                _bad(f"{name}: expected a contiguous int32 numpy array")
+            if t.size != n:
+                _bad(f"{name}: {t.size} elements, expected {n}")
+            addr.append(t.ctypes.data)
+        else:
+            at = _dev(t, name, T.i32)
+            if t.numel() != n:
+                _bad(f"{name}: {t.numel()} elements, expected {n}")
+            addr.append(at)
+    return addr
+
+
+def _rows_and_batch(parents, query_start):
+    try:
+        (rows,), (B,) = parents.shape, query_start.shape
+    except ValueError:
+        _bad("expected parents [tokens] and query_start [batch + 1]")
+    if B < 1:
+        _bad("query_start: empty")
+    return rows, B - 1
+
+
+def _mask_words(mask, rows):
+    """(address, words) of the masks of `rows` rows."""
+    shape = mask.shape
+    if len(shape) != 2 or shape[0] != rows:
+        _bad(f"mask: shape {tuple(shape)}, expected [{rows}][words]")
+    return _dev(mask, "mask", _torch().i64), shape[1]
+
+
+def tree_tables(h, parents, query_start, seq_lens, mask, positions=None, base=None, stream=None):
+    """What the nodes of drafted trees attend and where they stand: parents int32 [T] (a
+    node's parent within its request, -1: a root), query_start int32 [B + 1], seq_lens int32
+    [B] in; mask int64 [T][words] (64 nodes a word), positions int32 [T] and base int32 [B]
+    (tokens before the tree) out. Device tensors (numpy arrays for a host-only slice,
+    which only validates)."""
+    rows, B = _rows_and_batch(parents, query_start)
+    rec = _HANDLES.get(h)
+    host = rec[0] if rec else _host_only(h)
+    addr = _i32_args(host, (("parents", parents, rows), ("query_start", query_start, B + 1),
+                            ("seq_lens", seq_lens, B), ("positions", positions, rows),
+                            ("base", base, B)))
+    if host:
+        shape = mask.shape
+        if len(shape) != 2 or shape[0] != rows:
+            _bad(f"mask: shape {tuple(shape)}, expected [{rows}][words]")
+        at, words, st = None, shape[1], None
+    else:
+        (at, words), st = _mask_words(mask, rows), _stream(stream)
+    _check(_lib.ema_tree_tables(h, *addr[:3], rows, B, at, words, *addr[3:], st))
+
+
+def paged_tree_workspace(h, tokens, batch, num_q_heads, max_blocks):
+    return _size_call(_lib.ema_paged_tree_workspace, h, tokens, batch, num_q_heads, max_blocks)
+
+
+def paged_tree_attention(h, q, query_start, block_table, seq_lens, mask, out, scale=0.0,
+                         workspace=None, stream=None, full_weights=False):
+    """Attention of drafted nodes: mask int64 [T][words] says which of its request's nodes a
+    row attends beside all tokens before them (bit j: the node in the j-th of the request's
+    rows, which are its last tokens); the other arrays as in paged_prompt_attention."""
+    _attention_op(h, _lib.ema_paged_tree_attention, _lib.ema_paged_tree_workspace, 1, q,
+                  query_start, block_table, seq_lens, out, scale, None, None, 0.0, full_weights,
+                  workspace, stream, mask)
+
+
+def tree_accept(h, parents, query_start, drafted, choice, path, n_path, next_token,
+                root_choice=None, stream=None):
+    """The path of each tree that the model's choices confirm: parents, drafted (the nodes'
+    tokens), choice (the model's after them) int32 [T], query_start [B + 1], root_choice
+    int32 [B] (the model's choice before the tree; None: node 0 is accepted as it is) in; path
+    int32 [B][cap] (-1 behind the path), n_path and next_token int32 [B] out."""
+    rows, B = _rows_and_batch(parents, query_start)
+    shape = path.shape
+    if len(shape) != 2 or shape[0] != B:
+        _bad(f"path: shape {tuple(shape)}, expected [{B}][cap]")
+    rec = _HANDLES.get(h)
+    host = rec[0] if rec else _host_only(h)
+    addr = _i32_args(host, (("parents", parents, rows), ("query_start", query_start, B + 1),
+                            ("drafted", drafted, rows), ("choice", choice, rows),
+                            ("root_choice", root_choice, B), ("path", path, B * shape[1]),
+                            ("n_path", n_path, B), ("next_token", next_token, B)))
+    _check(_lib.ema_tree_accept(h, *addr[:5], rows, B, shape[1], *addr[5:],
+                                None if host else _stream(stream)))
+
+
+def kv_compact(h, block_table, base, keep, n_keep, new_lens=None, stream=None):
+    """Moves kept tokens together, in all layers and in place: token base[b] + k becomes what
+    token base[b] + keep[b][k] was, k < n_keep[b]; new_lens[b] = base[b] + n_keep[b].
+    block_table int32 [L][B][max_blocks] (unified ids), base, n_keep, new_lens int32
+    [B], keep int32 [B][cap], ascending."""
+    try:
+        (L, B, width), (_, cap) = block_table.shape, keep.shape
+    except ValueError:
+        _bad("expected block_table [L][B][max_blocks] and keep [B][cap]")
+    rec = _HANDLES.get(h)
+    host = rec[0] if rec else _host_only(h)
+    addr = _i32_args(host, (("block_table", block_table, L * B * width), ("base", base, B),
+                            ("keep", keep, B * cap), ("n_keep", n_keep, B),
+                            ("new_lens", new_lens, B)))
+    _check(_lib.ema_kv_compact(h, *addr[:4], L, B, width, cap, addr[4],
+                               None if host else _stream(stream)))
 
 
 # ---- slab management of the slice --------------------------------------------------
