@@ -30,9 +30,6 @@
 namespace ema {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * 64;
-
 // P of a tile in NP 16-bit parts whose sum keeps 8 (bf16) or 11 (f16) bits each.
 template <int NP>
 struct Weights {
@@ -52,280 +49,767 @@ __device__ __forceinline__ void put_weights(Weights<NP>& w, int ks, int q, float
   }
 }
 
-// A piece's values that are not finite: zeroed in the piece; ones in their places.
-template <bool BF16>
-__device__ __forceinline__ u32x4 take_not_finite(u32x4& v) {
-  constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u, kOne = BF16 ? 0x3f80u : 0x3c00u;
-  u32x4 ones;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool lo = (v[i] & kExp) == kExp, hi = ((v[i] >> 16) & kExp) == kExp;
-    ones[i] = (lo ? kOne : 0u) | (hi ? kOne << 16 : 0u);
-    v[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
-  }
-  return ones;
-}
+// Loads a tile of K or V into LDS, in the places of prompt_common.h. Its 16 pieces of 1 KiB are
+// shared out to RW waves; a lane's part of an address is the same for all of them but for the four
+// (K) or two (V) ways in which their 16-byte parts are turned, the rest is the wave's.
+template <int BSC, int RW>
+struct TileLoader {
+  static constexpr int kPieces = 16 / RW;
+  struct Blocks {
+    const char* at[4];                     // the blocks of the tile's 16-token groups
+  };
+  const char* local;
+  int64_t block_bytes, v_at;               // v_at: the head's V in a block
+  int shift, mask, last, k_at, row_bytes;
+  uint32_t k_lane[4], v_lane[2];
+  IdWindow window;
 
-template <bool BF16, int BSC, int NP, int RT>
-__global__ __launch_bounds__(kThreads, 1) void tree_kernel(TreeAttnArgs a) {
-  constexpr int kRows = 32 * RT;
-  constexpr uint32_t kOne = BF16 ? 0x3f80u : 0x3c00u;
-  // K and V of a tile per wave; at the end each wave's outputs
-  __shared__ __attribute__((aligned(16))) u32x4 s_kv[kWaves][2][kTilePieces];
-  __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
-  __shared__ int s_find[kFindScratch];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int col = lane & 31, half = lane >> 5;
-  const int G = a.q_heads / a.kv_heads;
-  const int kvh = int(blockIdx.x) % a.kv_heads;
-  const RowTile R = find_in_order<kThreads, kRows>(a, G, int(blockIdx.x) / a.kv_heads, s_find);
-  if (blockIdx.x == 0 && R.wrong > 0) atomicAdd(a.err_count, R.wrong);
-  if (R.b < 0) return;
-  if (R.first == 0 && kvh == 0 && tid == 0 && (R.len < R.n || R.len != R.given))
-    atomicAdd(a.err_count, 1);
-  const int base = R.len - R.n;            // tokens before the tree; negative: nodes without a place
-  const int tiles = (R.len + kKT - 1) / kKT;
-  const bool counts = kvh == 0 && R.first == 0;
-
-  // this lane's rows
-  int tok[RT], head[RT];
-  bool live[RT];
-  u32x4 q[RT][8];
+  // Once: what does not depend on the segment. rw: the wave's number among those of a tile.
+  __device__ __forceinline__ void init(const PromptArgs& a, int rw) {
+    const int lane = threadIdx.x & 63, l16 = lane >> 4;
+    local = a.local;
+    block_bytes = a.block_bytes;
+    shift = a.block_shift;
+    mask = a.block_size - 1;
+    row_bytes = a.block_size * 2;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int r = R.first + rt * 32 + col;
-    live[rt] = r < R.n * G;
-    tok[rt] = live[rt] ? r / G : 0;
-    head[rt] = kvh * G + (live[rt] ? r - tok[rt] * G : 0);
-    const char* p = a.q + (int64_t(R.row0 + tok[rt]) * a.q_stride + head[rt] * 128 + half * 8) * 2;
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) q[rt][ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
-  }
-
-  auto& s_k = s_kv[wave][0];
-  auto& s_v = s_kv[wave][1];
-  const uint32_t lds_k = lds_address(&s_k[0]), lds_v = lds_address(&s_v[0]);
-  Staging<BSC, 64> st;
-  typename Staging<BSC, 64>::Blocks at;
-
-  f32x16 o[RT][4], s[RT][2];
-  float m[RT], l[RT];                      // l: this lane's half of the tokens
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    m[rt] = -INFINITY;
-    l[rt] = 0.0f;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) o[rt][c] = f32x16{};
-  }
-  const int arow = score_row(col);
-  constexpr float kSlack = BF16 || NP == 1 ? 8.0f : 4.0f, kUp = BF16 ? 0.0f : 15.0f - kSlack;
-
-  // Which tokens of the tile from t0 on row rt attends, a bit each.
-  auto attended = [&](int rt, int t0) -> uint64_t {
-    if (!live[rt] || base + tok[rt] < 0) return 0;
-    const uint64_t* words = a.mask + int64_t(R.row0 + tok[rt]) * a.words;
-    const int j = t0 - base;               // the node at the tile's first token
-    uint64_t x;
-    if (j <= -64) {
-      x = ~0ull;
-    } else if (j < 0) {
-      x = (words[0] << -j) | ((1ull << -j) - 1ull);
-    } else {
-      const int w = j >> 6, by = j & 63;
-      x = w < a.words ? words[w] >> by : 0;
-      if (by > 0 && w + 1 < a.words) x |= words[w + 1] << (64 - by);
+    for (int i = 0; i < 4; ++i) {
+      const int row = ((rw * kPieces + i) & 3) * 4 + l16;
+      k_lane[i] = row * 256 + ((lane ^ row) & 15) * 16;
     }
-    const int left = R.len - t0;
-    if (left < 64) x &= (1ull << left) - 1ull;
-    if (st.window.bad != 0)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      constexpr int r = BSC / 8;           // pieces of a channel's row
+      const int turn = BSC == 64 ? i * 4 + l16 : BSC == 32 ? l16 : l16 & 1;
+      v_lane[i] = lane / r * row_bytes + ((lane % r) ^ turn) * 16;
+    }
+  }
+  __device__ __forceinline__ void open(const PromptArgs& a, int b, int kvh, int j, int end) {
+    last = (end - 1) >> shift;
+    k_at = kvh * 256 * a.block_size;
+    v_at = block_bytes / 2 + k_at;
+    window.open(a, b, (j * kKT) >> shift, last);
+  }
+  // Where tile j's tokens are; tiles in ascending order.
+  __device__ __forceinline__ Blocks blocks(int j) {
+    Blocks t;
+    const int first = (j * kKT) >> shift;
+    window.seek(min(first, last));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      t.at[i] = local + int64_t(window.get(min(first + i * 16 / BSC, last))) * block_bytes;
+    return t;
+  }
+  __device__ __forceinline__ void load_k(uint32_t to, int j, const Blocks& t, int rw) const {
+    const int in = k_at + (BSC == 64 ? ((j * kKT) & mask) * 256 : 0);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int x = rw * kPieces + i, row = (x >> 2) * 16 & (BSC - 1);
+      load_to_lds(pick(t, x >> 2) + in + row * 256, k_lane[i & 3], to + x * 1024);
+    }
+  }
+  __device__ __forceinline__ void load_v(uint32_t to, int j, const Blocks& t, int rw) const {
+    const int64_t in = v_at + (BSC == 64 ? ((j * kKT) & mask) * 2 : 0);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int x = rw * kPieces + i;
+      constexpr int per = BSC / 4;         // pieces of a block: 4, 8 or 16
+      const int group = x / per * (BSC / 16);
+      load_to_lds(pick(t, group) + in + int64_t(x % per * (64 / (BSC / 8))) * row_bytes,
+                  v_lane[BSC == 64 ? i & 1 : 0], to + x * 1024);
+    }
+  }
+  // (selected, not indexed: the array stays in registers)
+  static __device__ __forceinline__ const char* pick(const Blocks& t, int i) {
+    const char* lo = i & 1 ? t.at[1] : t.at[0];
+    const char* hi = i & 1 ? t.at[3] : t.at[2];
+    return i & 2 ? hi : lo;
+  }
+  // Which tokens of tile j are of blocks of the pool and before token `end`.
+  __device__ __forceinline__ uint64_t there(int j, int end) const {
+    const int t0 = j * kKT, n = end - t0;
+    uint64_t x = n < 64 ? (1ull << n) - 1ull : ~0ull;
+    if (window.bad != 0)
 #pragma unroll
       for (int i = 0; i < 4; ++i)          // 16 tokens, in one block
-        if (!st.window.good((t0 + 16 * i) >> a.block_shift)) x &= ~(0xffffull << (16 * i));
+        if (!window.good((t0 + 16 * i) >> shift)) x &= ~(0xffffull << (16 * i));
+    return x;
+  }
+  // In the pieces of V tile j that this lane has loaded: what is not `there` becomes 0, and so
+  // does what is not finite; whether there was any of that.
+  template <bool BF16>
+  __device__ __forceinline__ bool clean_v(u32x4* tile, uint64_t there, int rw) const {
+    constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u;
+    constexpr int r = BSC / 8, per = BSC / 4;
+    const int lane = threadIdx.x & 63, l16 = lane >> 4;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int x = rw * kPieces + i;
+      const int turn = BSC == 64 ? (i & 1) * 4 + l16 : BSC == 32 ? l16 : l16 & 1;
+      const uint32_t bits = uint32_t(there >> (x / per * BSC + ((lane % r) ^ turn) * 8));
+      u32x4 v = tile[x * 64 + lane];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] &= (bits >> (2 * k) & 1 ? 0xffffu : 0u) | (bits >> (2 * k + 1) & 1 ? 0xffff0000u : 0u);
+        const uint32_t drop = ((v[k] & kExp) == kExp ? 0xffffu : 0u) |
+                              ((v[k] >> 16 & kExp) == kExp ? 0xffff0000u : 0u);
+        any |= drop;
+        v[k] &= ~drop;
+      }
+      tile[x * 64 + lane] = v;
+    }
+    return any != 0;
+  }
+  // Counts the entries of tile j whose block begins there, before token `end`, and is not of the
+  // pool; one wave of those that see a sequence's tiles does. (window.bad takes whole windows, of
+  // which a part of the tiles holds some only.)
+  __device__ __forceinline__ void count_bad(const PromptArgs& a, int j, int end) const {
+    const int lane = threadIdx.x & 63, tok = j * kKT + lane * 16;
+    const bool bad = lane < kKT / 16 && tok < end && (tok & mask) == 0 && !window.good(tok >> shift);
+    const int n = __popcll(__ballot(bad));
+    if (n > 0 && lane == 0) atomicAdd(a.err_count, n);
+  }
+};
+
+// Tiles that a segment costs a workgroup beyond its own: its queries, its first tiles' way from
+// HBM, its merge.
+constexpr int kSegCost = 4;
+constexpr int kCus = 256;
+constexpr int kWholeTiles = 8;           // tables of at most so many tiles: items are not shared
+constexpr int kRecord = 6;               // ints: see Record
+constexpr int kJoinRows = 8;
+
+// An item: a row tile of one (request, KV head). What the join needs of one that several
+// workgroups share.
+struct Record {
+  int from, to;                          // its first workgroup (-1: not shared), its last one
+  int row0, rows, first, kvh;            // the request's first row, its rows, the tile's first
+};
+
+// How a call is cut: by its sizes alone.
+struct Cut {
+  int64_t bound;                         // items at most
+  int rows;                              // of an item
+  int grid;
+  int whole;                             // an item to a workgroup; else equal shares of all tiles
+};
+
+// Records are kept by item where there are no more of them than that, else by the workgroup in
+// which an item begins.
+__host__ __device__ __forceinline__ bool by_item(const Cut& c) { return c.bound <= 2 * c.grid; }
+
+// A run of tiles [j0, j1) of one item.
+struct Segment {
+  int b, row0, n, len, nt;               // the request, its rows in q, its tokens
+  int item, items;                       // of the request's
+  int index;                             // of all items
+  int j0, j1;
+};
+
+// The shapes of a workgroup: RW waves share a tile, 32 rows each, and kWaves / RW groups of such
+// waves take a segment's tiles in turn, each with kPlaces places of its own for tiles.
+template <int ROWS>
+struct Shape;
+template <>
+struct Shape<32> { static constexpr int kWaves = 4, kPlaces = 1, kPerCu = 1; };
+template <>
+struct Shape<64> { static constexpr int kWaves = 4, kPlaces = 1, kPerCu = 2; };
+template <>
+struct Shape<128> { static constexpr int kWaves = 4, kPlaces = 2, kPerCu = 2; };
+template <>
+struct Shape<256> { static constexpr int kWaves = 8, kPlaces = 4, kPerCu = 1; };
+
+template <bool BF16, int BSC, int NP, int ROWS>
+__global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeAttnArgs a, Cut cut) {
+  constexpr int kWaves = Shape<ROWS>::kWaves, kThreads = kWaves * 64, kPlaces = Shape<ROWS>::kPlaces;
+  constexpr int RW = ROWS / 32, kGroups = kWaves / RW, kRows = ROWS;
+  // The groups' K and V tiles; at a segment's end 16 KiB of each wave's outputs
+  __shared__ __attribute__((aligned(16))) u32x4 s_kv[kGroups * kPlaces][2][kTilePieces];
+  __shared__ float s_m[kWaves][32], s_l[kWaves][32];
+  __shared__ int64_t s_sum[kWaves][2], s_into;
+  __shared__ int s_start[2], s_odd[2];       // s_odd: 1 values that are not finite, 2 bad blocks
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int rw = wave % RW, group = wave / RW;
+  const int col = lane & 31, half = lane >> 5;
+  const int B = a.batch, G = a.q_heads / a.kv_heads, H = a.kv_heads;
+  const int wg = blockIdx.x, grid = gridDim.x;
+  const bool itemwise = by_item(cut);
+  float* const ws_ml = a.ws + int64_t(2) * grid * kRows * 128;
+  int32_t* const info = reinterpret_cast<int32_t*>(ws_ml + int64_t(2) * grid * kRows * 2);
+
+  // ---- the workgroup's range: equal shares of all items' tiles ---------------------------
+  auto clamp_len = [&](int len) { return max(0, min(len, a.max_blocks * a.block_size)); };
+  auto items_of = [&](int n, int len) { return len > 0 ? (n * G + kRows - 1) / kRows * H : 0; };
+  auto units_of = [&](int n, int len) {
+    return int64_t(items_of(n, len)) * (cut.whole ? 1 : (len + kKT - 1) / kKT + kSegCost);
+  };
+  const int per_t = (B + kThreads - 1) / kThreads;
+  const int b0 = min(B, tid * per_t), b1 = min(B, b0 + per_t);
+  int64_t units = 0, items = 0;
+  for (int b = b0; b < b1; ++b) {
+    int s, n;
+    const int wrong = row_range(a, b, s, n), given = a.seq_lens[b], len = clamp_len(given);
+    if (wg == 0 && wrong > 0) atomicAdd(a.err_count, 1);
+    if (wg == 0 && n > 0 && (len < n || len != given)) atomicAdd(a.err_count, 1);
+    units += units_of(n, len);
+    items += items_of(n, len);
+  }
+  int64_t incl[2] = {units, items};
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int64_t y = __shfl_up(incl[x], o);
+      if (lane >= o) incl[x] += y;
+    }
+  if (lane == 63) {
+    s_sum[wave][0] = incl[0];
+    s_sum[wave][1] = incl[1];
+  }
+  if (tid == 0) {
+    s_start[0] = -1;
+    s_odd[0] = s_odd[1] = 0;
+  }
+  __syncthreads();
+  int64_t before = incl[0] - units, index = incl[1] - items, U = 0, all_items = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) {
+      before += s_sum[w][0];
+      index += s_sum[w][1];
+    }
+    U += s_sum[w][0];
+    all_items += s_sum[w][1];
+  }
+  const int64_t per = cut.whole ? 1 : (U + grid - 1) / grid;
+  const int64_t u0 = wg * per, u1 = min(U, u0 + per);
+  for (int b = b0; b < b1; ++b) {
+    int s, n;
+    row_range(a, b, s, n);
+    const int len = clamp_len(a.seq_lens[b]);
+    const int64_t x = units_of(n, len);
+    if (u0 >= before && u0 < before + x) {
+      s_start[0] = b;
+      s_start[1] = int(index);
+      s_into = u0 - before;
+    }
+    before += x;
+    index += items_of(n, len);
+  }
+  if (!cut.whole && wg == 0 && tid == 0) info[0] = itemwise ? int(all_items) : grid;
+  if (!cut.whole && !itemwise && tid == 0) info[1 + wg * kRecord] = -1;
+  for (int b = wg; b < B; b += grid) {       // requests without tokens
+    if (a.seq_lens[b] > 0 && a.max_blocks > 0) continue;
+    int s, n;
+    row_range(a, b, s, n);
+    AttnArgs out;
+    out.out = a.out;
+    out.out_dtype = a.out_dtype;
+    out.out_vec = 1;
+    for (int64_t x = tid; x < int64_t(n) * a.q_heads * 32; x += kThreads)
+      store_out4(out, int64_t(s) * a.q_heads * 128 + 4 * x, out_f32x4{});
+  }
+  __syncthreads();
+  if (uniform(s_start[0]) < 0) return;
+
+  int64_t left = u1 - u0;                    // units of the range not yet handed out
+  auto take = [&](Segment& g, int r) {       // from unit r of the item (its cost first)
+    const int cost = max(0, kSegCost - r);
+    if (left <= cost) return false;
+    left -= cost;
+    g.j0 = max(0, r - kSegCost);
+    g.j1 = int(min(int64_t(g.nt), g.j0 + left));
+    left -= g.j1 - g.j0;
+    return true;
+  };
+  auto set_request = [&](Segment& g) {
+    int s, n;
+    row_range(a, g.b, s, n);
+    g.row0 = uniform(s);
+    g.n = uniform(n);
+    g.len = uniform(clamp_len(a.seq_lens[g.b]));
+    g.nt = (g.len + kKT - 1) / kKT;
+    g.items = items_of(g.n, g.len);
+  };
+  auto next_segment = [&](Segment& g) {
+    if (cut.whole || left <= kSegCost) return false;
+    ++g.index;
+    if (++g.item == g.items) {
+      g.item = 0;
+      do {
+        if (++g.b >= B) return false;
+        set_request(g);
+      } while (g.items == 0);
+    }
+    return take(g, 0);
+  };
+
+  // ---- a segment's rows and tiles ----------------------------------------------------------
+  int kvh = 0, first = 0, base = 0;          // of segment g; base: tokens before the nodes
+  int tok = -1;                              // the node of this lane's row, -1: no row
+  u32x4 q[8];
+  TileLoader<BSC, RW> st;
+  typename TileLoader<BSC, RW>::Blocks at;
+  st.init(a, rw);
+  auto load_q = [&](const Segment& g) {
+    const int tiles = g.items / H;
+    kvh = g.item / tiles;
+    first = (g.item - kvh * tiles) * kRows;
+    base = g.len - g.n;
+    const int r = first + rw * 32 + col;
+    const bool live = r < g.n * G;
+    const int node = live ? r / G : 0, h = live ? r - node * G : 0;
+    tok = live ? node : -1;
+    const char* p = a.q + (int64_t(g.row0 + node) * a.q_stride + (kvh * G + h) * 128 + half * 8) * 2;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
+  };
+
+  // Which tokens from t0 on a node attends, a bit each, but for those that are not there.
+  auto attended = [&](const Segment& g, int node, int t0) -> uint64_t {
+    const int before = g.len - g.n, j = t0 - before;   // j: the node at the first of them
+    if (node < 0 || before + node < 0) return 0;
+    if (j <= -64) return ~0ull;
+    const uint64_t* words = a.mask + int64_t(g.row0 + node) * a.words;
+    if (j < 0) return (words[0] << -j) | ((1ull << -j) - 1ull);
+    const int w = j >> 6, by = j & 63;
+    uint64_t x = w < a.words ? words[w] >> by : 0;
+    if (by > 0 && w + 1 < a.words) x |= words[w + 1] << (64 - by);
     return x;
   };
 
-  if (wave < tiles) {
-    st.open(a, R.b, kvh, wave, R.len);
-    at = st.blocks(wave);
-    st.load_k(lds_k, wave, at, 0);
-    st.load_v(lds_v, wave, at, 0);
+  // ---- a tile ------------------------------------------------------------------------------
+  f32x16 o[4], s[2];
+  float m, l;                                // l: this lane's half of the tokens
+  Weights<NP> w;
+  bool odd = false;                          // V that is not finite in tiles that are masked in part
+  const int arow = score_row(col);
+  constexpr float kSlack = BF16 || NP == 1 ? 8.0f : 4.0f, kUp = BF16 ? 0.0f : 15.0f - kSlack;
+  auto scores = [&](const u32x4* K) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
-      for (int ks = 0; ks < 8; ++ks) arrived(q[rt][ks]);
-  }
-  for (int j = wave; j < tiles; j += kWaves) {
-    const int t0 = j * kKT;
-    const bool more = j + kWaves < tiles;
-    const bool partly = t0 + kKT > base || st.window.bad != 0;
-    uint64_t sees[RT];
-    loads_arrived();
-    if (counts && st.window.bad != 0) st.count_bad(a, j, R.len);
+      for (int tt = 0; tt < 2; ++tt)
+        s[tt] = mfma32<BF16>(K[k_place(tt * 32 + arow, ks * 2 + half)], q[ks],
+                             ks == 0 ? f32x16{} : s[tt]);
+  };
+  auto hide = [&](const Segment& g, int j, uint64_t there) {
+    const uint64_t sees = attended(g, tok, j * kKT) & there;
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) sees[rt] = partly ? attended(rt, t0) : ~0ull;
+    for (int tt = 0; tt < 2; ++tt) {
+      const uint32_t bits = uint32_t(sees >> (tt * 32 + half * 8));
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        s[tt][i] = (bits >> ((i >> 3) * 16 + (i & 7))) & 1 ? s[tt][i] : -INFINITY;
+    }
+  };
+  auto softmax = [&] {
+    float mx = -INFINITY;
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-      for (int ks = 0; ks < 8; ++ks) {
-        const u32x4 k = s_k[k_place(tt * 32 + arow, ks * 2 + half)];
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[tt][i]);
+    mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
+    if (__ballot(mx > m + kSlack)) {
+      const float m_new = fmaxf(m, mx);
+      const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-          s[rt][tt] = mfma32<BF16>(k, q[rt][ks], ks == 0 ? f32x16{} : s[rt][tt]);
-      }
-    Weights<NP> w[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      if (partly) {
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          const uint32_t bits = uint32_t(sees[rt] >> (tt * 32 + half * 8));
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            s[rt][tt][i] = (bits >> ((i >> 3) * 16 + (i & 7))) & 1 ? s[rt][tt][i] : -INFINITY;
-        }
-      }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[rt][tt][i]);
-      mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
-      if (__ballot(mx > m[rt] + kSlack)) {
-        const float m_new = fmaxf(m[rt], mx);
-        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - m_new);
-        m[rt] = m_new;
-        l[rt] *= alpha;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) o[rt][c] *= alpha;
-      }
-      const float ref = m[rt] == -INFINITY ? 0.0f : m[rt] - kUp;
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          float p[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            p[e] = __builtin_amdgcn_exp2f(
-                fmaf(s[rt][ks >> 1][(ks & 1) * 8 + 2 * x + e], a.scale_log2, -ref));
-            l[rt] += p[e];
-          }
-          put_weights<BF16, NP>(w[rt], ks, x, p[0], p[1]);
-        }
+      for (int c = 0; c < 4; ++c) o[c] *= alpha;
     }
+    const float ref = m == -INFINITY ? 0.0f : m - kUp;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        float p[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(
+              fmaf(s[ks >> 1][(ks & 1) * 8 + 2 * x + e], a.scale_log2, -ref));
+          l += p[e];
+        }
+        put_weights<BF16, NP>(w, ks, x, p[0], p[1]);
+      }
+  };
+  auto values = [&](const u32x4* V) {
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        u32x4 v = s_v[v_place<BSC>(c * 32 + col, ks * 2 + half)];
-        if (partly && __ballot(not_finite<BF16>(v))) {
-          const u32x4 bad = take_not_finite<BF16>(v);
+        const u32x4 v = V[v_place<BSC>(c * 32 + col, ks * 2 + half)];
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            const uint32_t bits = uint32_t(sees[rt] >> (ks * 16 + half * 8));
-            u32x4 ones;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              ones[i] = (bits >> (2 * i) & 1 ? kOne : 0u) | (bits >> (2 * i + 1) & 1 ? kOne << 16 : 0u);
-            const f32x16 hit = mfma32<BF16>(bad, ones, f32x16{});
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[rt][c][i] = hit[i] > 0.0f ? NAN : o[rt][c][i];
-          }
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-          for (int n = 0; n < NP; ++n) o[rt][c] = mfma32<BF16>(v, w[rt].p[n][ks], o[rt][c]);
+        for (int n = 0; n < NP; ++n) o[c] = mfma32<BF16>(v, w.p[n][ks], o[c]);
       }
-    reads_done();
-    if (more) {
-      at = st.blocks(j + kWaves);
-      st.load_k(lds_k, j + kWaves, at, 0);
-      st.load_v(lds_v, j + kWaves, at, 0);
-    }
-  }
-
-  // ---- the waves' parts of a row -------------------------------------------------------
-  __syncthreads();
-  f32x4* const part = reinterpret_cast<f32x4*>(&s_kv[0][0][0]);
-  // Four channels 4f .. 4f + 3 of a wave's row, rows off each other's banks.
-  auto part_at = [&](int w, int r, int f) -> f32x4& {
-    return part[w * (2 * kTilePieces) + r * 32 + (f ^ (r & 31))];
   };
+  // A tile masked in part: by the nodes' mask, the request's end or blocks out of range.
+  auto is_partly = [&](int j) { return (j + 1) * kKT > base || st.window.bad != 0; };
+
+  auto tile = [&](int place, int v) -> u32x4* { return s_kv[group * kPlaces + place][v]; };
+  auto load_k = [&](int j, int place) { st.load_k(lds_address(tile(place, 0)), j, at, rw); };
+  auto load_v = [&](int j, int place) { st.load_v(lds_address(tile(place, 1)), j, at, rw); };
+  // This wave's part of V tile j has arrived: cleaned where some row masks some of it.
+  auto clean = [&](const Segment& g, int j, int place) {
+    if (is_partly(j)) odd |= st.template clean_v<BF16>(tile(place, 1), st.there(j, g.len), rw);
+  };
+  auto open = [&](const Segment& g) {        // the first tiles' loads
+    const int j = g.j0 + group;
+    if (j >= g.j1) return;
+    st.open(a, g.b, kvh, j, g.len);
+    at = st.blocks(j);
+    load_k(j, 0);
+    if constexpr (RW == 1 || kPlaces > 1) load_v(j, 0);
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const float sum = l[rt] + other_half(l[rt]);
+    for (int i = 1; i < kPlaces - 1; ++i)
+      if (j + i * kGroups < g.j1) {
+        at = st.blocks(j + i * kGroups);
+        load_k(j + i * kGroups, i);
+        load_v(j + i * kGroups, i);
+      }
+  };
+
+  Segment g;
+  g.b = uniform(s_start[0]);
+  g.index = uniform(s_start[1]);
+  set_request(g);
+  if (cut.whole) {
+    g.item = uniform(int(s_into));
+    g.j0 = 0;
+    g.j1 = g.nt;
+  } else {
+    const int64_t into = s_into;
+    const int each = g.nt + kSegCost;
+    g.item = uniform(int(into / each));
+    g.index += g.item;
+    if (!take(g, uniform(int(into - int64_t(g.item) * each))) && !next_segment(g)) return;
+  }
+  bool have = true;
+  int turn = 0;                              // whose s_odd is this segment's
+  load_q(g);
+  open(g);
+  while (have) {
+    m = -INFINITY;
+    l = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) arrived(q[ks]);
+    const bool counts = kvh == 0 && first == 0 && rw == 0;
+    const int turns = (g.j1 - g.j0 + kGroups - 1) / kGroups;
+    if constexpr (RW == 1) {
+      for (int j = g.j0 + group; j < g.j1; j += kGroups) {
+        const bool more = j + kGroups < g.j1;
+        if (counts && st.window.bad != 0) st.count_bad(a, j, g.len);
+        loads_arrived_but_16();              // V of this tile is still on its way
+        scores(tile(0, 0));
+        if (is_partly(j)) hide(g, j, st.there(j, g.len));
+        reads_done();
+        const bool partly = is_partly(j);
+        const uint64_t there = partly ? st.there(j, g.len) : 0;
+        if (more) {
+          at = st.blocks(j + kGroups);
+          load_k(j + kGroups, 0);
+        }
+        softmax();
+        if (more) loads_arrived_but_16();    // the next tile's K is still on its way
+        else loads_arrived();
+        if (partly) odd |= st.template clean_v<BF16>(tile(0, 1), there, 0);
+        values(tile(0, 1));
+        reads_done();
+        if (more) load_v(j + kGroups, 0);
+      }
+    } else if constexpr (kPlaces == 1) {
+      // K of a tile is on its way while the values of the tile before are weighed, V while its
+      // scores are; a barrier before each tells that it is there and that all are done with what
+      // its place held.
+      for (int i = 0; i < turns; ++i) {
+        const int j = g.j0 + group + i * kGroups;
+        const bool here = j < g.j1;
+        loads_arrived();
+        __syncthreads();
+        if (here) {
+          load_v(j, 0);
+          if (counts && st.window.bad != 0) st.count_bad(a, j, g.len);
+          scores(tile(0, 0));
+          if (is_partly(j)) hide(g, j, st.there(j, g.len));
+          softmax();
+          loads_arrived();
+          clean(g, j, 0);
+        }
+        __syncthreads();
+        if (here) {
+          if (j + kGroups < g.j1) {
+            at = st.blocks(j + kGroups);
+            load_k(j + kGroups, 0);
+          }
+          values(tile(0, 1));
+        }
+      }
+    } else {
+      // This tile's loads have arrived, everyone's do after the barrier, which also tells that
+      // all are done with the tile before: its place takes the tile kPlaces - 1 ahead.
+      int place = 0;
+      for (int i = 0; i < turns; ++i) {
+        const int j = g.j0 + group + i * kGroups, next = j + (kPlaces - 1) * kGroups;
+        const bool here = j < g.j1;
+        // (the newest ones are those of the next kPlaces - 2 tiles)
+        static_assert(kPlaces == 2 || (kPlaces - 2) * 2 * 16 / RW == 8, "");
+        if (kPlaces > 2 && next - kGroups < g.j1) loads_arrived_but_8();
+        else loads_arrived();
+        if (here) clean(g, j, place);
+        __syncthreads();
+        if (next < g.j1) {
+          const int to = place == 0 ? kPlaces - 1 : place - 1;
+          at = st.blocks(next);
+          load_k(next, to);
+          load_v(next, to);
+        }
+        if (here) {
+          if (counts && st.window.bad != 0) st.count_bad(a, j, g.len);
+          scores(tile(place, 0));
+          if (is_partly(j)) hide(g, j, st.there(j, g.len));
+          softmax();
+          values(tile(place, 1));
+        }
+        place = place == kPlaces - 1 ? 0 : place + 1;
+      }
+    }
+
+    // ---- the waves' parts of a row -----------------------------------------------------
+    if (__ballot(odd) && lane == 0) atomicOr(&s_odd[turn], st.window.bad != 0 ? 3 : 1);
+    odd = false;
+    __syncthreads();                         // all are done with their tiles
+    f32x4* const part = reinterpret_cast<f32x4*>(&s_kv[0][0][0]);
+    // Four channels 4f .. 4f + 3 of a wave's row, rows off each other's banks.
+    auto part_at = [&](int w, int r, int f) -> f32x4& {
+      return part[w * kTilePieces + r * 32 + (f ^ r)];
+    };
+    const float sum = l + other_half(l);
     if (half == 0) {
-      s_m[wave][rt * 32 + col] = m[rt];
-      s_l[wave][rt * 32 + col] = sum;
+      s_m[wave][col] = m;
+      s_l[wave][col] = sum;
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        part_at(wave, rt * 32 + col, c * 8 + i * 2 + half) =
-            f32x4{o[rt][c][4 * i], o[rt][c][4 * i + 1], o[rt][c][4 * i + 2], o[rt][c][4 * i + 3]};
+        part_at(wave, col, c * 8 + i * 2 + half) =
+            f32x4{o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
+    const Segment done = g;
+    const int done_first = first, done_kvh = kvh;
+    have = next_segment(g);
+    if (have) load_q(g);
+    __syncthreads();
+    const int odds = s_odd[turn];
+    turn ^= 1;
+    if (tid == 0) s_odd[turn] = 0;           // (read before the last barrier but one)
+    const bool begins = done.j0 == 0, ends = done.j1 == done.nt;
+    const int64_t slot = 2 * wg + (begins ? 1 : 0);
+    AttnArgs out;
+    out.out = a.out;
+    out.out_dtype = a.out_dtype;
+    out.out_vec = 1;
+    for (int x = tid; x < kRows * 32; x += kThreads) {
+      const int r = x >> 5, f = x & 31, w0 = r >> 5, wr = r & 31;
+      if (done_first + r >= done.n * G) break;
+      float M = -INFINITY, L = 0.0f;
+#pragma unroll
+      for (int y = 0; y < kGroups; ++y) M = fmaxf(M, s_m[y * RW + w0][wr]);
+      const float ref = M == -INFINITY ? 0.0f : M;
+      f32x4 O = f32x4{};
+#pragma unroll
+      for (int y = 0; y < kGroups; ++y) {
+        const float by = __builtin_amdgcn_exp2f(s_m[y * RW + w0][wr] - ref);
+        L = fmaf(by, s_l[y * RW + w0][wr], L);
+        O += part_at(y * RW + w0, wr, f) * by;
+      }
+      const int node = (done_first + r) / G, h = done_first + r - node * G;
+      if (odds != 0) {
+        // V was cleaned of what is not finite: a row that attends such a value gets NaN
+        const int32_t* row = a.table + int64_t(done.b) * a.max_blocks;
+        const int begin = max(done.j0 * kKT, odds & 2 ? 0 : (done.len - done.n) & ~(kKT - 1));
+        for (int t = begin; t < min(done.j1 * kKT, done.len); ++t) {
+          const int id = row[t >> a.block_shift];
+          if (!(attended(done, node, t & ~(kKT - 1)) >> (t & (kKT - 1)) & 1)) continue;
+          if (uint32_t(id) >= uint32_t(a.n_local)) continue;
+          const uint16_t* v = reinterpret_cast<const uint16_t*>(
+              a.local + int64_t(id) * a.block_bytes + a.block_bytes / 2) +
+              int64_t(done_kvh * 128 + 4 * f) * a.block_size + (t & (a.block_size - 1));
+          constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if ((v[i * a.block_size] & kExp) == kExp) O[i] = NAN;
+        }
+      }
+      if (!(begins && ends)) {
+        *reinterpret_cast<f32x4*>(a.ws + (slot * kRows + r) * 128 + 4 * f) = O;
+        if (f == 0) {
+          ws_ml[(slot * kRows + r) * 2] = M;
+          ws_ml[(slot * kRows + r) * 2 + 1] = L;
+        }
+        continue;
+      }
+      const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+      store_out4(out, (int64_t(done.row0 + node) * a.q_heads + done_kvh * G + h) * 128 + 4 * f,
+                 out_f32x4{O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv});
+    }
+    if (!cut.whole && begins && tid == 0 && (itemwise || !ends)) {
+      int32_t* const rec = info + 1 + (itemwise ? done.index : wg) * kRecord;
+      rec[0] = ends ? -1 : wg;
+      // a part: the range ends with this segment
+      rec[1] = int((u1 + (done.nt - done.j1) - 1) / per);
+      rec[2] = done.row0;
+      rec[3] = done.n * G;
+      rec[4] = done_first;
+      rec[5] = done_kvh;
+    }
+    __syncthreads();
+    if (have) open(g);
   }
-  __syncthreads();
+}
+
+// Joins the parts of shared items: 32 lanes to a row, four channels a lane; `share` such groups
+// of a workgroup take a row's parts in turn.
+__global__ __launch_bounds__(kJoinRows * 32) void tree_join(TreeAttnArgs a, int grid, int rows,
+                                                            int share) {
+  __shared__ __attribute__((aligned(16))) f32x4 s_o[kJoinRows][32];
+  __shared__ float s_m[kJoinRows], s_l[kJoinRows];
+  const float* ws_ml = a.ws + int64_t(2) * grid * rows * 128;
+  const int32_t* info = reinterpret_cast<const int32_t*>(ws_ml + int64_t(2) * grid * rows * 2);
+  if (int(blockIdx.x) >= info[0]) return;
+  const int32_t* rec = info + 1 + int(blockIdx.x) * kRecord;
+  const int w0 = rec[0];
+  if (w0 < 0) return;
+  const int n = rec[1] - w0 + 1, f = threadIdx.x & 31, group = threadIdx.x >> 5;
+  const int r = int(blockIdx.y) * (kJoinRows / share) + group / share;
+  const bool live = r < rows && rec[4] + r < rec[3];
+  float M = -INFINITY, L = 0.0f;
+  f32x4 O = f32x4{};
+  constexpr int kAtOnce = 4;
+  for (int i0 = group % share; live && i0 < n; i0 += kAtOnce * share) {
+    f32x4 po[kAtOnce];
+    float pm[kAtOnce], pl[kAtOnce];
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) {
+      const int i = min(i0 + y * share, n - 1);
+      const int64_t at = int64_t(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * rows + r;
+      po[y] = *reinterpret_cast<const f32x4*>(a.ws + at * 128 + 4 * f);
+      pm[y] = ws_ml[at * 2];
+      pl[y] = ws_ml[at * 2 + 1];
+    }
+#pragma unroll
+    for (int y = 0; y < kAtOnce; ++y) {
+      if (i0 + y * share >= n) break;
+      const float M_new = fmaxf(M, pm[y]);
+      const float ref = M_new == -INFINITY ? 0.0f : M_new;
+      const float d = __builtin_amdgcn_exp2f(M - ref), e = __builtin_amdgcn_exp2f(pm[y] - ref);
+      M = M_new;
+      L = L * d + pl[y] * e;
+      O = O * d + po[y] * e;
+    }
+  }
+  if (share > 1) {
+    s_o[group][f] = O;
+    if (f == 0) {
+      s_m[group] = M;
+      s_l[group] = L;
+    }
+    __syncthreads();
+    if (group % share != 0) return;
+    float top = -INFINITY;
+    for (int y = 0; y < share; ++y) top = fmaxf(top, s_m[group + y]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    L = 0.0f;
+    O = f32x4{};
+    for (int y = 0; y < share; ++y) {
+      const float d = __builtin_amdgcn_exp2f(s_m[group + y] - ref);
+      L = fmaf(d, s_l[group + y], L);
+      O += s_o[group + y][f] * d;
+    }
+  }
+  if (!live) return;
   AttnArgs out;
   out.out = a.out;
   out.out_dtype = a.out_dtype;
   out.out_vec = 1;
-  for (int x = tid; x < kRows * 32; x += kThreads) {
-    const int r = x >> 5, f = x & 31;
-    if (R.first + r >= R.n * G) break;
-    float M = -INFINITY, L = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][r]);
-    const float ref = M == -INFINITY ? 0.0f : M;
-    f32x4 O = f32x4{};
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float by = __builtin_amdgcn_exp2f(s_m[w][r] - ref);
-      L = fmaf(by, s_l[w][r], L);
-      O += part_at(w, r, f) * by;
-    }
-    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-    const int node = (R.first + r) / G, g = R.first + r - node * G;
-    store_out4(out, (int64_t(R.row0 + node) * a.q_heads + kvh * G + g) * 128 + 4 * f,
-               out_f32x4{O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv});
-  }
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  const int G = a.q_heads / a.kv_heads, node = (rec[4] + r) / G, h = rec[4] + r - node * G;
+  store_out4(out, (int64_t(rec[2] + node) * a.q_heads + rec[5] * G + h) * 128 + 4 * f,
+             out_f32x4{O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv});
 }
 
-int row_tiles(const PromptArgs& a) {
-  const int64_t rows = (int64_t(a.tokens) + a.batch - 1) / a.batch * (a.q_heads / a.kv_heads);
-  return rows <= 32 ? 1 : 2;
+Cut cut_of(const PromptArgs& a) {
+  Cut c;
+  const int64_t mean = (int64_t(a.tokens) + a.batch - 1) / a.batch * (a.q_heads / a.kv_heads);
+  c.rows = 32;
+  while (c.rows < 256 && c.rows < mean) c.rows *= 2;
+  c.bound = tile_bound(a, c.rows) * a.kv_heads;
+  // (the most that there can be tiles)
+  const int64_t tiles = (int64_t(a.max_blocks) * a.block_size + kKT - 1) / kKT;
+  const int64_t most_wgs = kCus * (c.rows == 64 ? Shape<64>::kPerCu : c.rows == 128 ? Shape<128>::kPerCu : 1);
+  c.whole = tiles <= kWholeTiles && c.bound <= 1 << 16;
+  c.grid = c.whole ? int(c.bound)
+                   : int(std::max<int64_t>(1, c.bound > most_wgs || tiles > most_wgs
+                                                  ? most_wgs
+                                                  : std::min(most_wgs, c.bound * tiles)));
+  return c;
 }
+int64_t records(const Cut& c) { return by_item(c) ? c.bound : c.grid; }
 
-template <bool BF16, int NP, int RT>
-void launch_sizes(const TreeAttnArgs& a, hipStream_t stream) {
-  const dim3 grid(unsigned(tile_bound(a, 32 * RT) * a.kv_heads));
+template <bool BF16, int NP, int ROWS>
+void launch_sizes(const TreeAttnArgs& a, const Cut& c, hipStream_t stream) {
+  const dim3 grid(unsigned(c.grid)), threads(Shape<ROWS>::kWaves * 64);
   if (a.block_size == 16)
-    hipLaunchKernelGGL((tree_kernel<BF16, 16, NP, RT>), grid, dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((tree_kernel<BF16, 16, NP, ROWS>), grid, threads, 0, stream, a, c);
   else if (a.block_size == 32)
-    hipLaunchKernelGGL((tree_kernel<BF16, 32, NP, RT>), grid, dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((tree_kernel<BF16, 32, NP, ROWS>), grid, threads, 0, stream, a, c);
   else
-    hipLaunchKernelGGL((tree_kernel<BF16, 64, NP, RT>), grid, dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((tree_kernel<BF16, 64, NP, ROWS>), grid, threads, 0, stream, a, c);
 }
 
 template <bool BF16, int NP>
-void launch_rows(const TreeAttnArgs& a, hipStream_t stream) {
-  if (row_tiles(a) == 1) launch_sizes<BF16, NP, 1>(a, stream);
-  else launch_sizes<BF16, NP, 2>(a, stream);
+void launch_rows(const TreeAttnArgs& a, const Cut& c, hipStream_t stream) {
+  switch (c.rows) {
+    case 32:
+      launch_sizes<BF16, NP, 32>(a, c, stream);
+      break;
+    case 64:
+      launch_sizes<BF16, NP, 64>(a, c, stream);
+      break;
+    case 128:
+      launch_sizes<BF16, NP, 128>(a, c, stream);
+      break;
+    default:
+      launch_sizes<BF16, NP, 256>(a, c, stream);
+  }
 }
 
 }  // namespace
 
-size_t tree_workspace(const PromptArgs&) { return 0; }
+size_t tree_workspace(const PromptArgs& a) {
+  const Cut c = cut_of(a);
+  if (c.whole) return 0;
+  return (size_t(2) * c.grid * c.rows * 130 + 1 + size_t(records(c)) * kRecord) * 4;
+}
 
 hipError_t launch_tree_attention(const TreeAttnArgs& a, hipStream_t stream) {
+  const Cut c = cut_of(a);
   if (a.dtype == 1) {
-    if (a.full) launch_rows<true, 3>(a, stream);
-    else launch_rows<true, 1>(a, stream);
+    if (a.full) launch_rows<true, 3>(a, c, stream);
+    else launch_rows<true, 1>(a, c, stream);
   } else {
-    if (a.full) launch_rows<false, 2>(a, stream);
-    else launch_rows<false, 1>(a, stream);
+    if (a.full) launch_rows<false, 2>(a, c, stream);
+    else launch_rows<false, 1>(a, c, stream);
   }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || c.whole) return e;
+  const int64_t recs = records(c);
+  // as many groups to a row as it has parts, roughly
+  const int share = recs * 8 <= c.grid ? 8 : recs * 3 <= c.grid ? 4 : 1;
+  hipLaunchKernelGGL(tree_join, dim3(unsigned(recs), unsigned(c.rows * share / kJoinRows)),
+                     dim3(kJoinRows * 32), 0, stream, a, c.grid, c.rows, share);
   return hipGetLastError();
 }
 
