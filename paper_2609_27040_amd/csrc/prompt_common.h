@@ -452,12 +452,13 @@ __device__ __forceinline__ void load_lane_to_lds(const char* p, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                  :: "s"(uniform(int(lds))), "v"(p) : "memory", "m0");
 }
-// All of the wave's loads but the newest 16 (8) have arrived.
+// All of the wave's loads but the newest 16 (N) have arrived.
 __device__ __forceinline__ void loads_arrived_but_16() {
   asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
 }
-__device__ __forceinline__ void loads_arrived_but_8() {
-  asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+template <int N>
+__device__ __forceinline__ void loads_arrived_but() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 // Nothing of the wave still reads LDS.
 __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }

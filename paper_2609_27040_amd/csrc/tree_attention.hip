@@ -460,14 +460,14 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     st.open(a, g.b, kvh, j, g.len);
     at = st.blocks(j);
     load_k(j, 0);
-    if constexpr (RW == 1 || kPlaces > 1) load_v(j, 0);
+    if constexpr (RW == 1) load_v(j, 0);
 #pragma unroll
-    for (int i = 1; i < kPlaces - 1; ++i)
-      if (j + i * kGroups < g.j1) {
-        at = st.blocks(j + i * kGroups);
-        load_k(j + i * kGroups, i);
-        load_v(j + i * kGroups, i);
-      }
+    for (int i = 1; i < kPlaces; ++i) {
+      load_v(j + (i - 1) * kGroups, i - 1);
+      if (j + i * kGroups >= g.j1) return;
+      at = st.blocks(j + i * kGroups);
+      load_k(j + i * kGroups, i);
+    }
   };
 
   Segment g;
@@ -520,59 +520,47 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
         reads_done();
         if (more) load_v(j + kGroups, 0);
       }
-    } else if constexpr (kPlaces == 1) {
-      // K of a tile is on its way while the values of the tile before are weighed, V while its
-      // scores are; a barrier before each tells that it is there and that all are done with what
-      // its place held.
-      for (int i = 0; i < turns; ++i) {
-        const int j = g.j0 + group + i * kGroups;
-        const bool here = j < g.j1;
-        loads_arrived();
-        __syncthreads();
-        if (here) {
-          load_v(j, 0);
-          if (counts && st.window.bad != 0) st.count_bad(a, j, g.len);
-          scores(tile(0, 0));
-          if (is_partly(j)) hide(g, j, st.there(j, g.len));
-          softmax();
-          loads_arrived();
-          clean(g, j, 0);
-        }
-        __syncthreads();
-        if (here) {
-          if (j + kGroups < g.j1) {
-            at = st.blocks(j + kGroups);
-            load_k(j + kGroups, 0);
-          }
-          values(tile(0, 1));
-        }
-      }
     } else {
-      // This tile's loads have arrived, everyone's do after the barrier, which also tells that
-      // all are done with the tile before: its place takes the tile kPlaces - 1 ahead.
+      // K of a tile is sent for as soon as all are done with the scores of the one whose place it
+      // takes, V with the product of that one's: both are on their way nearly all of the time. A
+      // barrier tells that loads have arrived for all, and that all are done with a place.
+      constexpr int kNewer = kPlaces == 1 ? 16 / RW : 2 * (kPlaces - 1) * 16 / RW;
       int place = 0;
       for (int i = 0; i < turns; ++i) {
-        const int j = g.j0 + group + i * kGroups, next = j + (kPlaces - 1) * kGroups;
-        const bool here = j < g.j1;
-        // (the newest ones are those of the next kPlaces - 2 tiles)
-        static_assert(kPlaces == 2 || (kPlaces - 2) * 2 * 16 / RW == 8, "");
-        if (kPlaces > 2 && next - kGroups < g.j1) loads_arrived_but_8();
+        const int j = g.j0 + group + i * kGroups, last = j + (kPlaces - 1) * kGroups;
+        const int before = place == 0 ? kPlaces - 1 : place - 1;
+        const bool here = j < g.j1, more = last + kGroups < g.j1;
+        if (kPlaces > 1 && last < g.j1) loads_arrived_but<kNewer>();
         else loads_arrived();
-        if (here) clean(g, j, place);
         __syncthreads();
-        if (next < g.j1) {
-          const int to = place == 0 ? kPlaces - 1 : place - 1;
-          at = st.blocks(next);
-          load_k(next, to);
-          load_v(next, to);
+        if (last < g.j1) {
+          // (blocks are looked up in ascending order: `at` is tile last's still)
+          load_v(last, before);
         }
         if (here) {
           if (counts && st.window.bad != 0) st.count_bad(a, j, g.len);
           scores(tile(place, 0));
           if (is_partly(j)) hide(g, j, st.there(j, g.len));
-          softmax();
-          values(tile(place, 1));
         }
+        reads_done();
+        if (kPlaces > 1) {
+          if (last < g.j1) loads_arrived_but<kNewer>();
+          else loads_arrived();
+          if (here) clean(g, j, place);
+        }
+        __syncthreads();
+        if (more) {
+          at = st.blocks(last + kGroups);
+          load_k(last + kGroups, place);
+        }
+        if (here) softmax();
+        if (kPlaces == 1) {
+          if (more) loads_arrived_but<kNewer>();
+          else loads_arrived();
+          if (here) clean(g, j, place);
+          __syncthreads();
+        }
+        if (here) values(tile(place, 1));
         place = place == kPlaces - 1 ? 0 : place + 1;
       }
     }
