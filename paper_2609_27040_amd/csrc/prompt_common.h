@@ -435,12 +435,18 @@ struct IdWindow {
 // 16 bytes a lane from `base` (uniform) + `off` straight into LDS, at byte `lds` (uniform)
 // + 16 * lane. Nothing is written to registers; loads_arrived() waits for all of the
 // wave's.
+// NT: streamed past the caches.
+template <bool NT = false>
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, uint32_t lds) {
   const uint64_t b = reinterpret_cast<uint64_t>(base);
   const uint64_t ub = uint64_t(uint32_t(uniform(int(uint32_t(b))))) |
                       uint64_t(uint32_t(uniform(int(uint32_t(b >> 32))))) << 32;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :: "s"(uniform(int(lds))), "v"(off), "s"(ub) : "memory", "m0");
+  if constexpr (NT)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+                 :: "s"(uniform(int(lds))), "v"(off), "s"(ub) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(uniform(int(lds))), "v"(off), "s"(ub) : "memory", "m0");
 }
 // The same from an address per lane; NT: streamed past the caches.
 template <bool NT>

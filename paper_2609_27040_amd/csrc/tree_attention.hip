@@ -105,7 +105,7 @@ struct TileLoader {
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int x = rw * kPieces + i, row = (x >> 2) * 16 & (BSC - 1);
-      load_to_lds(pick(t, x >> 2) + in + row * 256, k_lane[i & 3], to + x * 1024);
+      load_to_lds<true>(pick(t, x >> 2) + in + row * 256, k_lane[i & 3], to + x * 1024);
     }
   }
   __device__ __forceinline__ void load_v(uint32_t to, int j, const Blocks& t, int rw) const {
@@ -115,7 +115,7 @@ struct TileLoader {
       const int x = rw * kPieces + i;
       constexpr int per = BSC / 4;         // pieces of a block: 4, 8 or 16
       const int group = x / per * (BSC / 16);
-      load_to_lds(pick(t, group) + in + int64_t(x % per * (64 / (BSC / 8))) * row_bytes,
+      load_to_lds<true>(pick(t, group) + in + int64_t(x % per * (64 / (BSC / 8))) * row_bytes,
                   v_lane[BSC == 64 ? i & 1 : 0], to + x * 1024);
     }
   }
@@ -179,6 +179,7 @@ constexpr int kCus = 256;
 constexpr int kWholeTiles = 8;           // tables of at most so many tiles: items are not shared
 constexpr int kRecord = 6;               // ints: see Record
 constexpr int kJoinRows = 8;
+constexpr int kJoinGrid = 2048;          // workgroups of the join that run at once
 
 // An item: a row tile of one (request, KV head). What the join needs of one that several
 // workgroups share.
@@ -193,6 +194,10 @@ struct Cut {
   int rows;                              // of an item
   int grid;
   int whole;                             // an item to a workgroup; else equal shares of all tiles
+  int least;                             // units of a share at least: parts of few tiles cost more
+                                         // than they save
+  int uneven;                            // ... or whole items, where no workgroup has more than
+                                         // this many quarters of such a share
 };
 
 // Records are kept by item where there are no more of them than that, else by the workgroup in
@@ -228,6 +233,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   __shared__ __attribute__((aligned(16))) u32x4 s_kv[kGroups * kPlaces][2][kTilePieces];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
   __shared__ int64_t s_sum[kWaves][2], s_into;
+  __shared__ int s_most[kWaves];
   __shared__ int s_start[2], s_odd[2];       // s_odd: 1 values that are not finite, 2 bad blocks
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int rw = wave % RW, group = wave / RW;
@@ -242,11 +248,12 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   auto clamp_len = [&](int len) { return max(0, min(len, a.max_blocks * a.block_size)); };
   auto items_of = [&](int n, int len) { return len > 0 ? (n * G + kRows - 1) / kRows * H : 0; };
   auto units_of = [&](int n, int len) {
-    return int64_t(items_of(n, len)) * (cut.whole ? 1 : (len + kKT - 1) / kKT + kSegCost);
+    return int64_t(items_of(n, len)) * ((len + kKT - 1) / kKT + kSegCost);
   };
   const int per_t = (B + kThreads - 1) / kThreads;
   const int b0 = min(B, tid * per_t), b1 = min(B, b0 + per_t);
   int64_t units = 0, items = 0;
+  int most = 0;                              // units of an item
   for (int b = b0; b < b1; ++b) {
     int s, n;
     const int wrong = row_range(a, b, s, n), given = a.seq_lens[b], len = clamp_len(given);
@@ -254,6 +261,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     if (wg == 0 && n > 0 && (len < n || len != given)) atomicAdd(a.err_count, 1);
     units += units_of(n, len);
     items += items_of(n, len);
+    if (n > 0 && len > 0) most = max(most, (len + kKT - 1) / kKT + kSegCost);
   }
   int64_t incl[2] = {units, items};
 #pragma unroll
@@ -263,9 +271,11 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
       const int64_t y = __shfl_up(incl[x], o);
       if (lane >= o) incl[x] += y;
     }
+  most = wave_max(most);
   if (lane == 63) {
     s_sum[wave][0] = incl[0];
     s_sum[wave][1] = incl[1];
+    s_most[wave] = most;
   }
   if (tid == 0) {
     s_start[0] = -1;
@@ -281,14 +291,18 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     }
     U += s_sum[w][0];
     all_items += s_sum[w][1];
+    most = max(most, s_most[w]);
   }
-  const int64_t per = cut.whole ? 1 : (U + grid - 1) / grid;
-  const int64_t u0 = wg * per, u1 = min(U, u0 + per);
+  const int64_t share = max((U + grid - 1) / grid, int64_t(cut.least)), rounds = (all_items + grid - 1) / grid;
+  const bool whole = cut.whole || rounds * most * 4 <= share * cut.uneven;
+  const int64_t per = whole ? rounds : share;
+  const int64_t u0 = wg * per, u1 = min(whole ? all_items : U, u0 + per);
+  if (whole) before = index;
   for (int b = b0; b < b1; ++b) {
     int s, n;
     row_range(a, b, s, n);
     const int len = clamp_len(a.seq_lens[b]);
-    const int64_t x = units_of(n, len);
+    const int64_t x = whole ? items_of(n, len) : units_of(n, len);
     if (u0 >= before && u0 < before + x) {
       s_start[0] = b;
       s_start[1] = int(index);
@@ -297,7 +311,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     before += x;
     index += items_of(n, len);
   }
-  if (!cut.whole && wg == 0 && tid == 0) info[0] = itemwise ? int(all_items) : grid;
+  if (!cut.whole && wg == 0 && tid == 0) info[0] = whole ? 0 : itemwise ? int(all_items) : grid;
   if (!cut.whole && !itemwise && tid == 0) info[1 + wg * kRecord] = -1;
   for (int b = wg; b < B; b += grid) {       // requests without tokens
     if (a.seq_lens[b] > 0 && a.max_blocks > 0) continue;
@@ -313,8 +327,13 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   __syncthreads();
   if (uniform(s_start[0]) < 0) return;
 
-  int64_t left = u1 - u0;                    // units of the range not yet handed out
+  int64_t left = u1 - u0;                    // units (whole: items) not yet handed out
   auto take = [&](Segment& g, int r) {       // from unit r of the item (its cost first)
+    if (whole) {
+      g.j0 = 0;
+      g.j1 = g.nt;
+      return left-- > 0;
+    }
     const int cost = max(0, kSegCost - r);
     if (left <= cost) return false;
     left -= cost;
@@ -333,7 +352,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     g.items = items_of(g.n, g.len);
   };
   auto next_segment = [&](Segment& g) {
-    if (cut.whole || left <= kSegCost) return false;
+    if (left <= (whole ? 0 : kSegCost)) return false;
     ++g.index;
     if (++g.item == g.items) {
       g.item = 0;
@@ -474,13 +493,9 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   g.b = uniform(s_start[0]);
   g.index = uniform(s_start[1]);
   set_request(g);
-  if (cut.whole) {
-    g.item = uniform(int(s_into));
-    g.j0 = 0;
-    g.j1 = g.nt;
-  } else {
+  {
     const int64_t into = s_into;
-    const int each = g.nt + kSegCost;
+    const int each = whole ? 1 : g.nt + kSegCost;
     g.item = uniform(int(into / each));
     g.index += g.item;
     if (!take(g, uniform(int(into - int64_t(g.item) * each))) && !next_segment(g)) return;
@@ -643,7 +658,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
       store_out4(out, (int64_t(done.row0 + node) * a.q_heads + done_kvh * G + h) * 128 + 4 * f,
                  out_f32x4{O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv});
     }
-    if (!cut.whole && begins && tid == 0 && (itemwise || !ends)) {
+    if (!whole && begins && tid == 0 && (itemwise || !ends)) {
       int32_t* const rec = info + 1 + (itemwise ? done.index : wg) * kRecord;
       rec[0] = ends ? -1 : wg;
       // a part: the range ends with this segment
@@ -666,66 +681,71 @@ __global__ __launch_bounds__(kJoinRows * 32) void tree_join(TreeAttnArgs a, int 
   __shared__ float s_m[kJoinRows], s_l[kJoinRows];
   const float* ws_ml = a.ws + int64_t(2) * grid * rows * 128;
   const int32_t* info = reinterpret_cast<const int32_t*>(ws_ml + int64_t(2) * grid * rows * 2);
-  if (int(blockIdx.x) >= info[0]) return;
-  const int32_t* rec = info + 1 + int(blockIdx.x) * kRecord;
-  const int w0 = rec[0];
-  if (w0 < 0) return;
-  const int n = rec[1] - w0 + 1, f = threadIdx.x & 31, group = threadIdx.x >> 5;
-  const int r = int(blockIdx.y) * (kJoinRows / share) + group / share;
-  const bool live = r < rows && rec[4] + r < rec[3];
-  float M = -INFINITY, L = 0.0f;
-  f32x4 O = f32x4{};
-  constexpr int kAtOnce = 4;
-  for (int i0 = group % share; live && i0 < n; i0 += kAtOnce * share) {
-    f32x4 po[kAtOnce];
-    float pm[kAtOnce], pl[kAtOnce];
+  const int each = rows * share / kJoinRows, tasks = info[0] * each;
+  const int f = threadIdx.x & 31, group = threadIdx.x >> 5;
+  const int G = a.q_heads / a.kv_heads;
+  for (int task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const int32_t* rec = info + 1 + task / each * kRecord;
+    const int w0 = rec[0], n = rec[1] - w0 + 1;
+    const int r = task % each * (kJoinRows / share) + group / share;
+    if (w0 < 0 || rec[4] + r - group / share >= rec[3]) continue;      // (the same for all)
+    const bool live = rec[4] + r < rec[3];
+    float M = -INFINITY, L = 0.0f;
+    f32x4 O = f32x4{};
+    constexpr int kAtOnce = 4;
+    for (int i0 = group % share; live && i0 < n; i0 += kAtOnce * share) {
+      f32x4 po[kAtOnce];
+      float pm[kAtOnce], pl[kAtOnce];
 #pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) {
-      const int i = min(i0 + y * share, n - 1);
-      const int64_t at = int64_t(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * rows + r;
-      po[y] = *reinterpret_cast<const f32x4*>(a.ws + at * 128 + 4 * f);
-      pm[y] = ws_ml[at * 2];
-      pl[y] = ws_ml[at * 2 + 1];
-    }
+      for (int y = 0; y < kAtOnce; ++y) {
+        const int i = i0 + y * share;
+        if (i >= n) break;
+        const int64_t at = int64_t(i == 0 ? 2 * w0 + 1 : 2 * (w0 + i)) * rows + r;
+        po[y] = *reinterpret_cast<const f32x4*>(a.ws + at * 128 + 4 * f);
+        pm[y] = ws_ml[at * 2];
+        pl[y] = ws_ml[at * 2 + 1];
+      }
 #pragma unroll
-    for (int y = 0; y < kAtOnce; ++y) {
-      if (i0 + y * share >= n) break;
-      const float M_new = fmaxf(M, pm[y]);
-      const float ref = M_new == -INFINITY ? 0.0f : M_new;
-      const float d = __builtin_amdgcn_exp2f(M - ref), e = __builtin_amdgcn_exp2f(pm[y] - ref);
-      M = M_new;
-      L = L * d + pl[y] * e;
-      O = O * d + po[y] * e;
+      for (int y = 0; y < kAtOnce; ++y) {
+        if (i0 + y * share >= n) break;
+        const float M_new = fmaxf(M, pm[y]);
+        const float ref = M_new == -INFINITY ? 0.0f : M_new;
+        const float d = __builtin_amdgcn_exp2f(M - ref), e = __builtin_amdgcn_exp2f(pm[y] - ref);
+        M = M_new;
+        L = L * d + pl[y] * e;
+        O = O * d + po[y] * e;
+      }
     }
+    if (share > 1) {
+      __syncthreads();                       // the task before is done with them
+      s_o[group][f] = O;
+      if (f == 0) {
+        s_m[group] = M;
+        s_l[group] = L;
+      }
+      __syncthreads();
+      if (group % share != 0) continue;
+      float top = -INFINITY;
+      for (int y = 0; y < share; ++y) top = fmaxf(top, s_m[group + y]);
+      const float ref = top == -INFINITY ? 0.0f : top;
+      L = 0.0f;
+      O = f32x4{};
+      for (int y = 0; y < share; ++y) {
+        const float d = __builtin_amdgcn_exp2f(s_m[group + y] - ref);
+        L = fmaf(d, s_l[group + y], L);
+        O += s_o[group + y][f] * d;
+      }
+    }
+    if (!live) continue;
+    AttnArgs out;
+    out.out = a.out;
+    out.out_dtype = a.out_dtype;
+    out.out_vec = 1;
+    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+    const int node = (rec[4] + r) / G, h = rec[4] + r - node * G;
+    store_out4(out, (int64_t(rec[2] + node) * a.q_heads + rec[5] * G + h) * 128 + 4 * f,
+               out_f32x4{O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv});
   }
-  if (share > 1) {
-    s_o[group][f] = O;
-    if (f == 0) {
-      s_m[group] = M;
-      s_l[group] = L;
-    }
-    __syncthreads();
-    if (group % share != 0) return;
-    float top = -INFINITY;
-    for (int y = 0; y < share; ++y) top = fmaxf(top, s_m[group + y]);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    L = 0.0f;
-    O = f32x4{};
-    for (int y = 0; y < share; ++y) {
-      const float d = __builtin_amdgcn_exp2f(s_m[group + y] - ref);
-      L = fmaf(d, s_l[group + y], L);
-      O += s_o[group + y][f] * d;
-    }
-  }
-  if (!live) return;
-  AttnArgs out;
-  out.out = a.out;
-  out.out_dtype = a.out_dtype;
-  out.out_vec = 1;
-  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-  const int G = a.q_heads / a.kv_heads, node = (rec[4] + r) / G, h = rec[4] + r - node * G;
-  store_out4(out, (int64_t(rec[2] + node) * a.q_heads + rec[5] * G + h) * 128 + 4 * f,
-             out_f32x4{O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv});
 }
 
 Cut cut_of(const PromptArgs& a) {
@@ -736,6 +756,8 @@ Cut cut_of(const PromptArgs& a) {
   c.bound = tile_bound(a, c.rows) * a.kv_heads;
   // (the most that there can be tiles)
   const int64_t tiles = (int64_t(a.max_blocks) * a.block_size + kKT - 1) / kKT;
+  c.least = c.rows < 256 ? 6 : 12;
+  c.uneven = c.rows < 256 ? 8 : 5;
   const int64_t most_wgs = kCus * (c.rows == 64 ? Shape<64>::kPerCu : c.rows == 128 ? Shape<128>::kPerCu : 1);
   c.whole = tiles <= kWholeTiles && c.bound <= 1 << 16;
   c.grid = c.whole ? int(c.bound)
@@ -796,7 +818,8 @@ hipError_t launch_tree_attention(const TreeAttnArgs& a, hipStream_t stream) {
   const int64_t recs = records(c);
   // as many groups to a row as it has parts, roughly
   const int share = recs * 8 <= c.grid ? 8 : recs * 3 <= c.grid ? 4 : 1;
-  hipLaunchKernelGGL(tree_join, dim3(unsigned(recs), unsigned(c.rows * share / kJoinRows)),
+  const int64_t tasks = recs * (c.rows * share / kJoinRows);
+  hipLaunchKernelGGL(tree_join, dim3(unsigned(std::min<int64_t>(tasks, kJoinGrid))),
                      dim3(kJoinRows * 32), 0, stream, a, c.grid, c.rows, share);
   return hipGetLastError();
 }
