@@ -230,6 +230,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   constexpr int kWaves = Shape<ROWS>::kWaves, kThreads = kWaves * 64, kPlaces = Shape<ROWS>::kPlaces;
   constexpr int RW = ROWS / 32, kGroups = kWaves / RW, kRows = ROWS;
   // The groups' K and V tiles; at a segment's end 16 KiB of each wave's outputs
+  static_assert(kGroups * kPlaces * 2 >= kWaves, "the outputs take the tiles' place");
   __shared__ __attribute__((aligned(16))) u32x4 s_kv[kGroups * kPlaces][2][kTilePieces];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
   __shared__ int64_t s_sum[kWaves][2], s_into;
@@ -239,7 +240,9 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   const int rw = wave % RW, group = wave / RW;
   const int col = lane & 31, half = lane >> 5;
   const int B = a.batch, G = a.q_heads / a.kv_heads, H = a.kv_heads;
-  const int wg = blockIdx.x, grid = gridDim.x;
+  // Workgroups go round the eight XCDs: an XCD's take items that follow each other.
+  const int grid = gridDim.x, id = blockIdx.x;
+  const int wg = grid % 8 == 0 ? id % 8 * (grid / 8) + id / 8 : id;
   const bool itemwise = by_item(cut);
   float* const ws_ml = a.ws + int64_t(2) * grid * kRows * 128;
   int32_t* const info = reinterpret_cast<int32_t*>(ws_ml + int64_t(2) * grid * kRows * 2);
@@ -294,7 +297,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     most = max(most, s_most[w]);
   }
   const int64_t share = max((U + grid - 1) / grid, int64_t(cut.least)), rounds = (all_items + grid - 1) / grid;
-  const bool whole = cut.whole || rounds * most * 4 <= share * cut.uneven;
+  const bool whole = cut.whole || rounds * most * 4 <= share * (rounds == 1 ? cut.uneven : 5);
   const int64_t per = whole ? rounds : share;
   const int64_t u0 = wg * per, u1 = min(whole ? all_items : U, u0 + per);
   if (whole) before = index;
@@ -463,6 +466,47 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
         for (int n = 0; n < NP; ++n) o[c] = mfma32<BF16>(v, w.p[n][ks], o[c]);
       }
   };
+  // The tile before's values weighed and this one's scores, in one run of products whose operands
+  // are read ahead.
+  auto products = [&](bool pv, const u32x4* V, bool qk, const u32x4* K) {
+    constexpr int kAhead = NP == 3 ? 4 : 6;
+    auto read_k = [&](int i) { return K[k_place((i & 1) * 32 + arow, (i >> 1) * 2 + half)]; };
+    __builtin_amdgcn_s_setprio(1);
+    u32x4 f[16], ahead[kAhead];
+    if (pv) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = V[v_place<BSC>((i & 3) * 32 + col, (i >> 2) * 2 + half)];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) ahead[i] = read_k(i);     // not used where !qk
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int n = 0; n < NP; ++n) o[i & 3] = mfma32<BF16>(f[i], w.p[n][i >> 2], o[i & 3]);
+      EMA_SCHED_LDS_READ(kAhead);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        EMA_SCHED_MFMA(NP);
+        EMA_SCHED_LDS_READ(1);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) ahead[i] = read_k(i);
+    }
+    if (qk) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i] = i < kAhead ? ahead[i] : read_k(i);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        s[i & 1] = mfma32<BF16>(f[i], q[i >> 1], i < 2 ? f32x16{} : s[i & 1]);
+#pragma unroll
+      for (int i = 0; i < 16 - kAhead; ++i) {
+        EMA_SCHED_MFMA(1);
+        EMA_SCHED_LDS_READ(1);
+      }
+      EMA_SCHED_MFMA(kAhead);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
   // A tile masked in part: by the nodes' mask, the request's end or blocks out of range.
   auto is_partly = [&](int j) { return (j + 1) * kKT > base || st.window.bad != 0; };
 
@@ -480,8 +524,9 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     at = st.blocks(j);
     load_k(j, 0);
     if constexpr (RW == 1) load_v(j, 0);
+    constexpr int kFirst = RW == 8 ? kPlaces - 1 : kPlaces;
 #pragma unroll
-    for (int i = 1; i < kPlaces; ++i) {
+    for (int i = 1; i < kFirst; ++i) {
       load_v(j + (i - 1) * kGroups, i - 1);
       if (j + i * kGroups >= g.j1) return;
       at = st.blocks(j + i * kGroups);
@@ -535,6 +580,47 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
         reads_done();
         if (more) load_v(j + kGroups, 0);
       }
+    } else if constexpr (RW == 8) {
+      // The eight waves are two groups, one of each to a SIMD, that take turns: while one has the
+      // matrix cores (products), the other works its scores into weights and sends for later tiles,
+      // V of the next but one and K of the one after it, into the places that the turns before were
+      // the last to read. The second group is one turn behind.
+      constexpr int kTurn = 2 * 16 / RW;     // a wave's loads of a turn
+      const int late = wave >= kWaves / 2 ? 1 : 0;
+      auto place = [&](int j) { return (j - g.j0) & (kPlaces - 1); };
+      auto send = [&](int j) {               // for V of tile j + 2 and K of j + 3
+        if (j + 2 < g.j1) load_v(j + 2, place(j + 2));
+        if (j + 3 < g.j1) {
+          at = st.blocks(j + 3);
+          load_k(j + 3, place(j + 3));
+        }
+      };
+      auto arrive = [&](int j) {             // V of tile j, K of j + 1
+        if (j >= g.j1) return;
+        if (j + 3 < g.j1) loads_arrived_but<2 * kTurn>();
+        else loads_arrived();
+        clean(g, j, place(j));
+        if (counts && st.window.bad != 0) st.count_bad(a, j, g.len);
+      };
+      if (g.j0 + 2 < g.j1) loads_arrived_but<2 * kTurn>();
+      else loads_arrived();
+      __syncthreads();
+      if (late) {
+        send(g.j0);
+        arrive(g.j0);
+        __syncthreads();
+      }
+      for (int j = g.j0; j < g.j1; ++j) {
+        products(j > g.j0, tile(place(j - 1), 1), true, tile(place(j), 0));
+        __syncthreads();
+        send(j + late);
+        if (is_partly(j)) hide(g, j, st.there(j, g.len));
+        softmax();
+        arrive(j + late);
+        __syncthreads();
+      }
+      products(true, tile(place(g.j1 - 1), 1), false, tile(0, 0));
+      if (!late) __syncthreads();
     } else {
       // K of a tile is sent for as soon as all are done with the scores of the one whose place it
       // takes, V with the product of that one's: both are on their way nearly all of the time. A
@@ -756,7 +842,7 @@ Cut cut_of(const PromptArgs& a) {
   c.bound = tile_bound(a, c.rows) * a.kv_heads;
   // (the most that there can be tiles)
   const int64_t tiles = (int64_t(a.max_blocks) * a.block_size + kKT - 1) / kKT;
-  c.least = c.rows < 256 ? 6 : 12;
+  c.least = c.rows < 256 ? 6 : 8;
   c.uneven = c.rows < 256 ? 8 : 5;
   const int64_t most_wgs = kCus * (c.rows == 64 ? Shape<64>::kPerCu : c.rows == 128 ? Shape<128>::kPerCu : 1);
   c.whole = tiles <= kWholeTiles && c.bound <= 1 << 16;
