@@ -17,7 +17,9 @@ layer); the swap of a layer group copies whole slab runs into a staging image.
 
 ``Chunk`` holds the tables of a step in which sequences gain several tokens at
 once (prompts): ``PagedKVCache.chunk`` has them built on the GPU, and the cache's
-``store``, ``prompt_attention`` and ``diff_prompt_attention`` go by them.
+``store``, ``prompt_attention`` and ``diff_prompt_attention`` go by them. ``Tree`` is
+the chunk of a step whose new tokens are drafted trees: ``tree_attention`` goes by
+its masks, ``accept`` and ``commit`` keep the path that the model confirms.
 
 Both expose the same step interface (``groups``, ``group``, ``staging_slots``,
 ``prefetch_group``, ``attention``), which ``step.StepRunner`` drives.
@@ -88,8 +90,46 @@ class Chunk:
             return
         self._users.add(raw)
         there = ema.torch_stream(raw)
-        for t in (self.block_table, self.slots, self.starts, *self.prefetch, *self.writeback):
+        for t in self._tables():
             t.record_stream(there)
+
+    def _tables(self):
+        return self.block_table, self.slots, self.starts, *self.prefetch, *self.writeback
+
+
+class Tree(Chunk):
+    """The tables of one step of a ``PagedKVCache`` whose sequences' last tokens are the
+    nodes of drafted trees: ``parents`` gives each sequence's (int arrays; a node's parent
+    within its sequence, -1 for a root; empty for none). Beside a chunk's tables, on the
+    device: ``mask`` [T][words] (which nodes a node attends), ``positions`` [T] (where it
+    stands in its sequence) and ``base`` [B] (the tokens before the tree)."""
+
+    _own = ()
+
+    def __init__(self, cache, parents, stream=None):
+        trees = [np.asarray(p, dtype=np.int64).reshape(-1) for p in parents]
+        for p in trees:
+            if (p < -1).any() or (p >= np.arange(len(p))).any():
+                raise ValueError("parents: each below its node, -1 for a root")
+        super().__init__(cache, [len(p) for p in trees], stream)
+        words = max(1, -(-max(map(len, trees), default=0) // 64))
+        self.parents = _dev(np.concatenate(trees + [np.zeros(0, np.int64)]))
+        i32 = dict(dtype=torch.int32, device="cuda")
+        self.mask = torch.empty((self.T, words), dtype=torch.int64, device="cuda")
+        self.positions, self.base = torch.empty(self.T, **i32), torch.empty(len(trees), **i32)
+        self._own = (self.parents, self.mask, self.positions, self.base)
+        here = torch.cuda.current_stream()
+        if stream is not None:
+            there = ema.torch_stream(stream)
+            if there != here:
+                there.wait_stream(here)
+                for t in self._own:
+                    t.record_stream(there)
+        ema.tree_tables(cache.h, self.parents, self.starts, cache.lens_dev, self.mask,
+                        self.positions, self.base, stream=stream)
+
+    def _tables(self):
+        return (*super()._tables(), *self._own)
 
 
 class PagedKVCache:
@@ -260,6 +300,43 @@ class PagedKVCache:
         chunk.used_on(stream)
         ema.slice_writeback(self.h, chunk.writeback[0][l], chunk.writeback[1][l],
                             chunk.n_writeback[l], stream=stream)
+
+    # ---- drafted trees ---------------------------------------------------------------------
+    def tree(self, parents, stream=None):
+        """The tables of a step whose sequences' last tokens are the nodes of drafted trees
+        (``self.lens`` counts them already; their blocks are allocated)."""
+        return Tree(self, parents, stream)
+
+    def tree_attention(self, l, tree, q, out, stream=None, full_weights=False):
+        tree.used_on(stream)
+        ema.paged_tree_attention(self.h, q, tree.starts, tree.block_table[l], self.lens_dev,
+                                 tree.mask, out, full_weights=full_weights, stream=stream)
+
+    def accept(self, tree, drafted, choice, cap=None, root_choice=None, stream=None):
+        """(path [B][cap], its lengths [B], the tokens after it [B]) of each tree that the
+        model's choices confirm, as in ``ema.tree_accept``; int32 device tensors."""
+        tree.used_on(stream)
+        cap = max(1, int(tree.new.max(initial=1))) if cap is None else int(cap)
+        with torch.cuda.stream(ema.torch_stream(stream)):
+            path, n, after = (torch.empty(s, dtype=torch.int32, device="cuda")
+                              for s in ((self.B, cap), (self.B,), (self.B,)))
+        ema.tree_accept(self.h, tree.parents, tree.starts, drafted, choice, path, n, after,
+                        root_choice=root_choice, stream=stream)
+        return path, n, after
+
+    def commit(self, tree, path, n_path, stream=None):
+        """Keeps the nodes of each sequence's path (ascending) of its tree: their K and V follow
+        the tokens before it in every layer, and the lengths are those tokens and the path.
+        Works on the canonical tables, so the layers' writebacks come before it. Waits for
+        the lengths, which the host keeps too."""
+        tree.used_on(stream)
+        there = ema.torch_stream(stream)
+        with torch.cuda.stream(there):
+            lens = torch.empty(self.B, dtype=torch.int32, device="cuda")
+            ema.kv_compact(self.h, self.tables_dev, tree.base, path, n_path, new_lens=lens,
+                           stream=stream)
+            self.lens_dev.copy_(lens)
+            self.lens = lens.cpu().numpy().astype(np.int64)
 
     def new_token_kv(self, seed=0):
         """One new token's K and V per sequence (device, the cache dtype),

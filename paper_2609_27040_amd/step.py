@@ -6,7 +6,8 @@ decode attention runs for each of the group's layers (section 2.3: a layer is
 not needed again until every other layer has run, which is the window the
 swap of the next group overlaps; section 4.2.2: swaps are issued at layer
 group boundaries into a swap buffer of one group). ``run_chunk`` orders a step
-that brings many tokens of a sequence at once. ``capture_ops`` and
+that brings many tokens of a sequence at once, ``run_tree`` one whose new tokens are
+drafted trees. ``capture_ops`` and
 ``capture_step`` record a one-stream step as a HIP graph. ``BlockedTimer``
 times a library call that also does host work.
 """
@@ -165,6 +166,19 @@ def run_chunk(w, chunk, layer, stream=None):
         w.store(l, chunk, k_new, v_new, stream=stream)
         w.prompt_attention(l, chunk, q, out, stream=stream)
         w.writeback_chunk(l, chunk, stream=stream)
+
+
+def run_tree(w, tree, layer, stream=None):
+    """The layers of a step whose new tokens are drafted trees (``w.tree``), in the order of
+    ``run_chunk``: each node attends the tokens before its tree and the nodes above it.
+    What the model then chooses after the nodes goes to ``w.accept``, the path to
+    ``w.commit``."""
+    for l in range(w.L):
+        w.prefetch_chunk(l, tree, stream=stream)
+        q, k_new, v_new, out = layer(l)
+        w.store(l, tree, k_new, v_new, stream=stream)
+        w.tree_attention(l, tree, q, out, stream=stream)
+        w.writeback_chunk(l, tree, stream=stream)
 
 
 def capture_ops(runner, ops):
