@@ -130,6 +130,16 @@ int attn_sizes(const AttnCall& c) {
   const int64_t tiles = int64_t(c.max_blocks) * c.h->shape.block_size / 32 + 8;
   if (!c.chunks && c.batch * tiles * (hkv / 2) >= (int64_t(1) << 31))
     return inval(c.what, "batch * max_blocks too large");
+  if (c.tree && c.tokens > 0 && c.batch > 0) {
+    ema::PromptArgs a{};
+    a.tokens = c.tokens;
+    a.batch = c.batch;
+    a.q_heads = c.num_q_heads;
+    a.kv_heads = hkv;
+    a.block_size = c.h->shape.block_size;
+    a.max_blocks = c.max_blocks;
+    if (!ema::tree_fits(a)) return inval(c.what, "tokens or batch times max_blocks too large");
+  }
   return EMA_OK;
 }
 

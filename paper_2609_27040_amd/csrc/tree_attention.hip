@@ -179,7 +179,19 @@ constexpr int kCus = 256;
 constexpr int kWholeTiles = 8;           // tables of at most so many tiles: items are not shared
 constexpr int kRecord = 6;               // ints: see Record
 constexpr int kJoinRows = 8;
-constexpr int kJoinGrid = 2048;          // workgroups of the join that run at once
+constexpr int kJoinGrid = 4096;          // workgroups of the join that run at once
+
+// Inclusive prefix sum over the wave's 64 lanes, by DPP moves: within rows of 16 lanes, then
+// the row totals carried over.
+__device__ __forceinline__ int wave_inclusive_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);    // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // lane 15 of rows 0, 2 to 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // lane 31 to rows 2, 3
+  return x;
+}
 
 // An item: a row tile of one (request, KV head). What the join needs of one that several
 // workgroups share.
@@ -233,8 +245,8 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   static_assert(kGroups * kPlaces * 2 >= kWaves, "the outputs take the tiles' place");
   __shared__ __attribute__((aligned(16))) u32x4 s_kv[kGroups * kPlaces][2][kTilePieces];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
-  __shared__ int64_t s_sum[kWaves][2], s_into;
-  __shared__ int s_most[kWaves];
+  __shared__ int s_sum[kWaves][2], s_into, s_most[kWaves];
+  __shared__ float s_roughly[kWaves];
   __shared__ int s_start[2], s_odd[2];       // s_odd: 1 values that are not finite, 2 bad blocks
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int rw = wave % RW, group = wave / RW;
@@ -251,41 +263,40 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   auto clamp_len = [&](int len) { return max(0, min(len, a.max_blocks * a.block_size)); };
   auto items_of = [&](int n, int len) { return len > 0 ? (n * G + kRows - 1) / kRows * H : 0; };
   auto units_of = [&](int n, int len) {
-    return int64_t(items_of(n, len)) * ((len + kKT - 1) / kKT + kSegCost);
+    return items_of(n, len) * ((len + kKT - 1) / kKT + kSegCost);
   };
   const int per_t = (B + kThreads - 1) / kThreads;
   const int b0 = min(B, tid * per_t), b1 = min(B, b0 + per_t);
-  int64_t units = 0, items = 0;
-  int most = 0;                              // units of an item
+  int units = 0, items = 0, most = 0;        // most: units of an item
+  float roughly = 0.0f;                      // the units
   for (int b = b0; b < b1; ++b) {
     int s, n;
     const int wrong = row_range(a, b, s, n), given = a.seq_lens[b], len = clamp_len(given);
     if (wg == 0 && wrong > 0) atomicAdd(a.err_count, 1);
     if (wg == 0 && n > 0 && (len < n || len != given)) atomicAdd(a.err_count, 1);
-    units += units_of(n, len);
+    const int x = units_of(n, len);
+    units = int(uint32_t(units) + uint32_t(x));
+    roughly += float(x);
     items += items_of(n, len);
     if (n > 0 && len > 0) most = max(most, (len + kKT - 1) / kKT + kSegCost);
   }
-  int64_t incl[2] = {units, items};
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int64_t y = __shfl_up(incl[x], o);
-      if (lane >= o) incl[x] += y;
-    }
+  int incl[2] = {wave_inclusive_sum(units), wave_inclusive_sum(items)};
   most = wave_max(most);
   if (lane == 63) {
     s_sum[wave][0] = incl[0];
     s_sum[wave][1] = incl[1];
     s_most[wave] = most;
   }
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) roughly += __shfl_xor(roughly, x);
+  if (lane == 0) s_roughly[wave] = roughly;
   if (tid == 0) {
     s_start[0] = -1;
     s_odd[0] = s_odd[1] = 0;
   }
   __syncthreads();
-  int64_t before = incl[0] - units, index = incl[1] - items, U = 0, all_items = 0;
+  int before = incl[0] - units, index = incl[1] - items, U = 0, all_items = 0;
+  float total = 0.0f;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     if (w < wave) {
@@ -295,26 +306,32 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     U += s_sum[w][0];
     all_items += s_sum[w][1];
     most = max(most, s_most[w]);
+    total += s_roughly[w];
   }
-  const int64_t share = max((U + grid - 1) / grid, int64_t(cut.least)), rounds = (all_items + grid - 1) / grid;
-  const bool whole = cut.whole || rounds * most * 4 <= share * (rounds == 1 ? cut.uneven : 5);
-  const int64_t per = whole ? rounds : share;
-  const int64_t u0 = wg * per, u1 = min(whole ? all_items : U, u0 + per);
+  if (total > 1.5f * (1 << 30)) {            // requests of many rows in common, by bad starts
+    if (!cut.whole && wg == 0 && tid == 0) info[0] = 0;
+    return;
+  }
+  const int share = max((U - 1) / grid + 1, cut.least), rounds = (all_items + grid - 1) / grid;
+  const bool whole = cut.whole || int64_t(rounds) * most * 4 <= int64_t(share) * (rounds == 1 ? cut.uneven : 5);
+  const int per = whole ? rounds : share, all = whole ? all_items : U;
+  // (a range may begin past the last unit: compared without adding to it)
+  const int u0 = int(min(int64_t(wg) * per, int64_t(all))), u1 = u0 + min(per, all - u0);
   if (whole) before = index;
   for (int b = b0; b < b1; ++b) {
     int s, n;
     row_range(a, b, s, n);
     const int len = clamp_len(a.seq_lens[b]);
-    const int64_t x = whole ? items_of(n, len) : units_of(n, len);
-    if (u0 >= before && u0 < before + x) {
+    const int x = whole ? items_of(n, len) : units_of(n, len);
+    if (u0 >= before && u0 - before < x) {
       s_start[0] = b;
-      s_start[1] = int(index);
+      s_start[1] = index;
       s_into = u0 - before;
     }
     before += x;
     index += items_of(n, len);
   }
-  if (!cut.whole && wg == 0 && tid == 0) info[0] = whole ? 0 : itemwise ? int(all_items) : grid;
+  if (!cut.whole && wg == 0 && tid == 0) info[0] = whole ? 0 : itemwise ? int(min(int64_t(all_items), cut.bound)) : grid;
   if (!cut.whole && !itemwise && tid == 0) info[1 + wg * kRecord] = -1;
   for (int b = wg; b < B; b += grid) {       // requests without tokens
     if (a.seq_lens[b] > 0 && a.max_blocks > 0) continue;
@@ -330,7 +347,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   __syncthreads();
   if (uniform(s_start[0]) < 0) return;
 
-  int64_t left = u1 - u0;                    // units (whole: items) not yet handed out
+  int left = u1 - u0;                        // units (whole: items) not yet handed out
   auto take = [&](Segment& g, int r) {       // from unit r of the item (its cost first)
     if (whole) {
       g.j0 = 0;
@@ -341,7 +358,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     if (left <= cost) return false;
     left -= cost;
     g.j0 = max(0, r - kSegCost);
-    g.j1 = int(min(int64_t(g.nt), g.j0 + left));
+    g.j1 = min(g.nt, g.j0 + left);
     left -= g.j1 - g.j0;
     return true;
   };
@@ -539,11 +556,10 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   g.index = uniform(s_start[1]);
   set_request(g);
   {
-    const int64_t into = s_into;
-    const int each = whole ? 1 : g.nt + kSegCost;
-    g.item = uniform(int(into / each));
+    const int into = uniform(s_into), each = whole ? 1 : g.nt + kSegCost;
+    g.item = uniform(into / each);
     g.index += g.item;
-    if (!take(g, uniform(int(into - int64_t(g.item) * each))) && !next_segment(g)) return;
+    if (!take(g, into - g.item * each) && !next_segment(g)) return;
   }
   bool have = true;
   int turn = 0;                              // whose s_odd is this segment's
@@ -744,11 +760,11 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
       store_out4(out, (int64_t(done.row0 + node) * a.q_heads + done_kvh * G + h) * 128 + 4 * f,
                  out_f32x4{O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv});
     }
-    if (!whole && begins && tid == 0 && (itemwise || !ends)) {
+    if (!whole && begins && tid == 0 && (itemwise ? done.index < cut.bound : !ends)) {
       int32_t* const rec = info + 1 + (itemwise ? done.index : wg) * kRecord;
       rec[0] = ends ? -1 : wg;
       // a part: the range ends with this segment
-      rec[1] = int((u1 + (done.nt - done.j1) - 1) / per);
+      rec[1] = (u1 + (done.nt - done.j1) - 1) / per;
       rec[2] = done.row0;
       rec[3] = done.n * G;
       rec[4] = done_first;
@@ -842,7 +858,7 @@ Cut cut_of(const PromptArgs& a) {
   c.bound = tile_bound(a, c.rows) * a.kv_heads;
   // (the most that there can be tiles)
   const int64_t tiles = (int64_t(a.max_blocks) * a.block_size + kKT - 1) / kKT;
-  c.least = c.rows < 256 ? 6 : 8;
+  c.least = c.rows < 256 ? 6 : 4;
   c.uneven = c.rows < 256 ? 8 : 5;
   const int64_t most_wgs = kCus * (c.rows == 64 ? Shape<64>::kPerCu : c.rows == 128 ? Shape<128>::kPerCu : 1);
   c.whole = tiles <= kWholeTiles && c.bound <= 1 << 16;
@@ -883,6 +899,11 @@ void launch_rows(const TreeAttnArgs& a, const Cut& c, hipStream_t stream) {
 }
 
 }  // namespace
+
+bool tree_fits(const PromptArgs& a) {
+  const int64_t tiles = (int64_t(a.max_blocks) * a.block_size + kKT - 1) / kKT;
+  return (tile_bound(a, 32) * a.kv_heads) * (tiles + kSegCost) < int64_t(1) << 30;
+}
 
 size_t tree_workspace(const PromptArgs& a) {
   const Cut c = cut_of(a);

@@ -40,6 +40,8 @@ struct TreeAttnArgs : PromptArgs {
   const uint64_t* mask;        // [tokens][words]
   int32_t words;
 };
+// Whether the items' tiles, all added up, are below 2^30 (sizes of a launch set).
+bool tree_fits(const PromptArgs& a);
 size_t tree_workspace(const PromptArgs& a);
 hipError_t launch_tree_attention(const TreeAttnArgs& a, hipStream_t stream);
 

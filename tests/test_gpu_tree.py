@@ -388,6 +388,26 @@ def test_bad_starts_and_lengths_are_counted(ema):
         c.close()
 
 
+@pytest.mark.parametrize("B", [40, 2000])
+def test_requests_of_the_same_rows(ema, B):
+    """Starts that go up and down give every second request all rows: more items than the sizes
+    allow for. They are counted, and the rows hold what one of them makes of them."""
+    c = SmallCache(ema, [700, 600] * (B // 2), 2, 16, "bf16", seed=54) if B < 100 else \
+        SmallCache(ema, [20] * B, 2, 16, "bf16", seed=54)
+    try:
+        q, mask = dev16(c.queries(60, 4), "bf16"), full((60, 1), -1, torch.int64)
+        starts = np.zeros(B + 1, np.int64)
+        starts[1::2] = 60
+        o = torch.full((60, 4, D), 7.0, device="cuda")
+        ema.paged_tree_attention(c.h, q, i32(starts), c.table_dev, c.lens_dev, mask, o)
+        errors = ema.slice_device_errors(c.h)
+        # the descending ones; where there are more rows than tokens, the others too
+        assert errors == B // 2 + (0 if B < 100 else B // 2)
+        assert torch.isfinite(o).all()
+    finally:
+        c.close()
+
+
 def test_more_nodes_than_tokens(ema):
     """Rows at negative positions give zeros, the others attend the nodes that are there."""
     k = Case(ema, [40, 3], [6, 7], (4, 2), 16, "bf16", seed=11, kind="chain")

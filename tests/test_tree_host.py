@@ -158,6 +158,8 @@ def test_attention_is_validated_on_the_host(host):
                                         (1 << 27, 1, 4, 1)):
         assert size(h, tokens, batch, heads, width, ctypes.byref(n)) == ema.ERR_INVAL
     assert size(h, 5, 1, 4, 1, None) == ema.ERR_INVAL
+    assert size(h, 65535, 65535, 4, 1 << 15, ctypes.byref(n)) == ema.ERR_INVAL   # tiles: 32 bits
+    assert size(h, 65535, 65535, 4, 1 << 14, ctypes.byref(n)) == ema.OK
 
 
 def test_arrays_of_another_rank_or_type(host):
