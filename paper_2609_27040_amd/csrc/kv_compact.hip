@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kThreads, 8) void compact_short(CompactArgs a, int 
   __shared__ Place s_src[kShort], s_dst[kShort];
   __shared__ int s_moves;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int part = blockIdx.x, parts = gridDim.x, b = b0 + blockIdx.y, l = l0 + blockIdx.z;
+  const int part = blockIdx.x, parts = gridDim.x, b = b0 + blockIdx.z, l = l0 + blockIdx.y;
   const Layout at(a.pools);
   const List list(a, l, b);
   if (part == 0 && l == 0) list.report(a, b, kThreads);
@@ -217,8 +217,26 @@ __global__ __launch_bounds__(kThreads + 64, 4) void compact_long(CompactArgs a, 
   const bool maker = wave == kMovers;
   const Layout at(a.pools);
   const int h = int(blockIdx.x) >> 1, ch0 = (int(blockIdx.x) & 1) * kHalf;
-  const int b = b0 + blockIdx.y, l = l0 + blockIdx.z;
+  const int l = l0 + blockIdx.y;
   const bool counts = blockIdx.x == 0;
+  // The longest lists first: they take the longest, and what is left over at the end of the launch
+  // should be short ones.
+  int b = b0 + blockIdx.z;
+  if (a.batch <= kThreads) {
+    int32_t* const counted = reinterpret_cast<int32_t*>(s_v);
+    const int mine = tid < a.batch ? a.n_keep[tid] : 0;
+    if (tid < a.batch) counted[tid] = mine;
+    __syncthreads();
+    int rank = 0;
+    if (tid < a.batch) {
+      for (int i = 0; i < a.batch; ++i)
+        rank += counted[i] > mine || (counted[i] == mine && i < tid);
+      if (rank == b0 + int(blockIdx.z)) s_first = tid;
+    }
+    __syncthreads();
+    b = uniform(s_first);
+    __syncthreads();
+  }
   const List list(a, l, b);
   if (counts && l == 0) list.report(a, b, kThreads + 64);
   // the first entry that moves: all before it stay
@@ -388,7 +406,7 @@ hipError_t launch(Kernel kernel, const CompactArgs& a, int parts, int threads, h
   const int layers = std::max(1, std::min(a.layers, (1 << 22) / (parts * batch)));
   for (int l = 0; l < a.layers; l += layers)
     for (int b = 0; b < a.batch; b += batch) {
-      hipLaunchKernelGGL(kernel, dim3(parts, std::min(batch, a.batch - b), std::min(layers, a.layers - l)),
+      hipLaunchKernelGGL(kernel, dim3(parts, std::min(layers, a.layers - l), std::min(batch, a.batch - b)),
                          dim3(threads), 0, stream, a, l, b);
       if (const hipError_t e = hipGetLastError()) return e;
     }
