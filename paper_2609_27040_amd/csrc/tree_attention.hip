@@ -245,9 +245,8 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   static_assert(kGroups * kPlaces * 2 >= kWaves, "the outputs take the tiles' place");
   __shared__ __attribute__((aligned(16))) u32x4 s_kv[kGroups * kPlaces][2][kTilePieces];
   __shared__ float s_m[kWaves][32], s_l[kWaves][32];
-  __shared__ int s_sum[kWaves][2], s_into, s_most[kWaves];
-  __shared__ float s_roughly[kWaves];
-  __shared__ int s_start[2], s_odd[2];       // s_odd: 1 values that are not finite, 2 bad blocks
+  __shared__ int s_sum[kWaves][2], s_most[kWaves], s_flags[kWaves], s_row[ROWS];
+  __shared__ int s_start[6], s_odd[2];       // s_odd: 1 values that are not finite, 2 bad blocks
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int rw = wave % RW, group = wave / RW;
   const int col = lane & 31, half = lane >> 5;
@@ -269,15 +268,19 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   const int b0 = min(B, tid * per_t), b1 = min(B, b0 + per_t);
   int units = 0, items = 0, most = 0;        // most: units of an item
   float roughly = 0.0f;                      // the units
+  int row0 = 0, n = 0, len = 0;              // of the thread's last request; mostly its only one
+  bool wrong = false, empty = false;         // bad starts; a request without tokens
   for (int b = b0; b < b1; ++b) {
-    int s, n;
-    const int wrong = row_range(a, b, s, n), given = a.seq_lens[b], len = clamp_len(given);
-    if (wg == 0 && wrong > 0) atomicAdd(a.err_count, 1);
+    const int bad = row_range(a, b, row0, n), given = a.seq_lens[b];
+    len = clamp_len(given);
+    if (wg == 0 && bad > 0) atomicAdd(a.err_count, 1);
     if (wg == 0 && n > 0 && (len < n || len != given)) atomicAdd(a.err_count, 1);
     const int x = units_of(n, len);
     units = int(uint32_t(units) + uint32_t(x));
     roughly += float(x);
     items += items_of(n, len);
+    wrong |= bad > 0;
+    empty |= n > 0 && len == 0;
     if (n > 0 && len > 0) most = max(most, (len + kKT - 1) / kKT + kSegCost);
   }
   int incl[2] = {wave_inclusive_sum(units), wave_inclusive_sum(items)};
@@ -287,16 +290,14 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     s_sum[wave][1] = incl[1];
     s_most[wave] = most;
   }
-#pragma unroll
-  for (int x = 32; x > 0; x >>= 1) roughly += __shfl_xor(roughly, x);
-  if (lane == 0) s_roughly[wave] = roughly;
+  const int flags = (__ballot(wrong) ? 1 : 0) | (__ballot(empty) ? 2 : 0);
+  if (lane == 0) s_flags[wave] = flags;
   if (tid == 0) {
     s_start[0] = -1;
     s_odd[0] = s_odd[1] = 0;
   }
   __syncthreads();
-  int before = incl[0] - units, index = incl[1] - items, U = 0, all_items = 0;
-  float total = 0.0f;
+  int before = incl[0] - units, index = incl[1] - items, U = 0, all_items = 0, flagged = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     if (w < wave) {
@@ -306,11 +307,20 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     U += s_sum[w][0];
     all_items += s_sum[w][1];
     most = max(most, s_most[w]);
-    total += s_roughly[w];
+    flagged |= s_flags[w];
   }
-  if (total > 1.5f * (1 << 30)) {            // requests of many rows in common, by bad starts
-    if (!cut.whole && wg == 0 && tid == 0) info[0] = 0;
-    return;
+  if (flagged & 1) {                         // requests of many rows in common, by bad starts
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) roughly += __shfl_xor(roughly, x);
+    __syncthreads();
+    if (lane == 0) s_m[wave][0] = roughly;
+    __syncthreads();
+    float total = 0.0f;
+    for (int w = 0; w < kWaves; ++w) total += s_m[w][0];
+    if (total > 1.5f * (1 << 30)) {
+      if (!cut.whole && wg == 0 && tid == 0) info[0] = 0;
+      return;
+    }
   }
   const int share = max((U - 1) / grid + 1, cut.least), rounds = (all_items + grid - 1) / grid;
   const bool whole = cut.whole || int64_t(rounds) * most * 4 <= int64_t(share) * (rounds == 1 ? cut.uneven : 5);
@@ -319,21 +329,25 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   const int u0 = int(min(int64_t(wg) * per, int64_t(all))), u1 = u0 + min(per, all - u0);
   if (whole) before = index;
   for (int b = b0; b < b1; ++b) {
-    int s, n;
-    row_range(a, b, s, n);
-    const int len = clamp_len(a.seq_lens[b]);
+    if (per_t > 1) {
+      row_range(a, b, row0, n);
+      len = clamp_len(a.seq_lens[b]);
+    }
     const int x = whole ? items_of(n, len) : units_of(n, len);
     if (u0 >= before && u0 - before < x) {
       s_start[0] = b;
       s_start[1] = index;
-      s_into = u0 - before;
+      s_start[2] = row0;
+      s_start[3] = n;
+      s_start[4] = len;
+      s_start[5] = u0 - before;
     }
     before += x;
     index += items_of(n, len);
   }
   if (!cut.whole && wg == 0 && tid == 0) info[0] = whole ? 0 : itemwise ? int(min(int64_t(all_items), cut.bound)) : grid;
   if (!cut.whole && !itemwise && tid == 0) info[1 + wg * kRecord] = -1;
-  for (int b = wg; b < B; b += grid) {       // requests without tokens
+  for (int b = wg; flagged & 2 && b < B; b += grid) {      // requests without tokens
     if (a.seq_lens[b] > 0 && a.max_blocks > 0) continue;
     int s, n;
     row_range(a, b, s, n);
@@ -362,12 +376,10 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     left -= g.j1 - g.j0;
     return true;
   };
-  auto set_request = [&](Segment& g) {
-    int s, n;
-    row_range(a, g.b, s, n);
+  auto set_request = [&](Segment& g, int s, int n, int len) {
     g.row0 = uniform(s);
     g.n = uniform(n);
-    g.len = uniform(clamp_len(a.seq_lens[g.b]));
+    g.len = uniform(len);
     g.nt = (g.len + kKT - 1) / kKT;
     g.items = items_of(g.n, g.len);
   };
@@ -378,7 +390,9 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
       g.item = 0;
       do {
         if (++g.b >= B) return false;
-        set_request(g);
+        int s, n;
+        row_range(a, g.b, s, n);
+        set_request(g, s, n, clamp_len(a.seq_lens[g.b]));
       } while (g.items == 0);
     }
     return take(g, 0);
@@ -386,7 +400,8 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
 
   // ---- a segment's rows and tiles ----------------------------------------------------------
   int kvh = 0, first = 0, base = 0;          // of segment g; base: tokens before the nodes
-  int tok = -1;                              // the node of this lane's row, -1: no row
+  int tok = -1, out_row = -1;                // the node of this lane's row, its row of out; -1: none
+  const uint64_t inverse = (1ull << 32) / G + 1;         // x * inverse >> 32 = x / G for x < 2^16
   u32x4 q[8];
   TileLoader<BSC, RW> st;
   typename TileLoader<BSC, RW>::Blocks at;
@@ -396,10 +411,11 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     kvh = g.item / tiles;
     first = (g.item - kvh * tiles) * kRows;
     base = g.len - g.n;
-    const int r = first + rw * 32 + col;
+    const int r = first + rw * 32 + col, node0 = first / G, x = first - node0 * G + rw * 32 + col;
     const bool live = r < g.n * G;
-    const int node = live ? r / G : 0, h = live ? r - node * G : 0;
+    const int node = live ? node0 + int(x * inverse >> 32) : 0, h = live ? r - node * G : 0;
     tok = live ? node : -1;
+    out_row = live ? (g.row0 + node) * a.q_heads + kvh * G + h : -1;
     const char* p = a.q + (int64_t(g.row0 + node) * a.q_stride + (kvh * G + h) * 128 + half * 8) * 2;
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) q[ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
@@ -554,9 +570,9 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
   Segment g;
   g.b = uniform(s_start[0]);
   g.index = uniform(s_start[1]);
-  set_request(g);
+  set_request(g, s_start[2], s_start[3], s_start[4]);
   {
-    const int into = uniform(s_into), each = whole ? 1 : g.nt + kSegCost;
+    const int into = uniform(s_start[5]), each = whole ? 1 : g.nt + kSegCost;
     g.item = uniform(into / each);
     g.index += g.item;
     if (!take(g, into - g.item * each) && !next_segment(g)) return;
@@ -695,6 +711,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     if (half == 0) {
       s_m[wave][col] = m;
       s_l[wave][col] = sum;
+      if (group == 0) s_row[rw * 32 + col] = out_row;
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -718,7 +735,8 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     out.out_vec = 1;
     for (int x = tid; x < kRows * 32; x += kThreads) {
       const int r = x >> 5, f = x & 31, w0 = r >> 5, wr = r & 31;
-      if (done_first + r >= done.n * G) break;
+      const int row = s_row[r];
+      if (row < 0) break;
       float M = -INFINITY, L = 0.0f;
 #pragma unroll
       for (int y = 0; y < kGroups; ++y) M = fmaxf(M, s_m[y * RW + w0][wr]);
@@ -730,13 +748,13 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
         L = fmaf(by, s_l[y * RW + w0][wr], L);
         O += part_at(y * RW + w0, wr, f) * by;
       }
-      const int node = (done_first + r) / G, h = done_first + r - node * G;
       if (odds != 0) {
+        const int node = (done_first + r) / G;
         // V was cleaned of what is not finite: a row that attends such a value gets NaN
-        const int32_t* row = a.table + int64_t(done.b) * a.max_blocks;
+        const int32_t* ids = a.table + int64_t(done.b) * a.max_blocks;
         const int begin = max(done.j0 * kKT, odds & 2 ? 0 : (done.len - done.n) & ~(kKT - 1));
         for (int t = begin; t < min(done.j1 * kKT, done.len); ++t) {
-          const int id = row[t >> a.block_shift];
+          const int id = ids[t >> a.block_shift];
           if (!(attended(done, node, t & ~(kKT - 1)) >> (t & (kKT - 1)) & 1)) continue;
           if (uint32_t(id) >= uint32_t(a.n_local)) continue;
           const uint16_t* v = reinterpret_cast<const uint16_t*>(
@@ -757,7 +775,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
         continue;
       }
       const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-      store_out4(out, (int64_t(done.row0 + node) * a.q_heads + done_kvh * G + h) * 128 + 4 * f,
+      store_out4(out, int64_t(row) * 128 + 4 * f,
                  out_f32x4{O[0] * inv, O[1] * inv, O[2] * inv, O[3] * inv});
     }
     if (!whole && begins && tid == 0 && (itemwise ? done.index < cut.bound : !ends)) {

@@ -683,22 +683,30 @@ def paged_diff_prompt_attention(h, q, query_start, block_table, seq_lens, lam, o
 
 def _i32_args(host, arrays):
     """Addresses of int32 arrays (name, array or None, elements it must have)."""
-    T = _torch() if not host else None
+    if not host:
+        T, addr = _torch(), []
+        Tensor, (int32,) = T.Tensor, T.i32
+        for name, t, n in arrays:
+            if t is None:
+                addr.append(None)
+            elif type(t) is Tensor and t.is_cuda and t.dtype is int32 and t.numel() == n and \
+                    t.is_contiguous():
+                addr.append(t.data_ptr())
+            else:
+                addr.append(_dev(t, name, T.i32))
+                if t.numel() != n:
+                    _bad(f"{name}: {t.numel()} elements, expected {n}")
+        return addr
     addr = []
     for name, t, n in arrays:
         if t is None:
             addr.append(None)
-        elif host:
+        else:
             if not isinstance(t, np.ndarray) or t.dtype != np.int32 or not t.flags.c_contiguous:
                 _bad(f"{name}: expected a contiguous int32 numpy array")
             if t.size != n:
                 _bad(f"{name}: {t.size} elements, expected {n}")
             addr.append(t.ctypes.data)
-        else:
-            at = _dev(t, name, T.i32)
-            if t.numel() != n:
-                _bad(f"{name}: {t.numel()} elements, expected {n}")
-            addr.append(at)
     return addr
 
 
