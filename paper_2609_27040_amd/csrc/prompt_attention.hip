@@ -38,25 +38,6 @@ constexpr int kThreads = kWaves * 64;
 constexpr int kRows = kWaves * 32;
 constexpr int kRing = 3;                 // staged tiles
 
-// P of a tile in NP 16-bit parts whose sum keeps 8 (bf16) or 11 (f16) bits each.
-template <int NP>
-struct Weights {
-  u32x4 p[NP][4];        // [part][16 tokens]
-};
-
-template <bool BF16, int NP>
-__device__ __forceinline__ void put_weights(Weights<NP>& w, int ks, int q, float x, float y) {
-#pragma unroll
-  for (int n = 0; n < NP; ++n) {
-    const uint32_t u = pack16<BF16>(x, y);
-    w.p[n][ks][q] = u;
-    if (n + 1 < NP) {
-      x -= low16<BF16>(u);
-      y -= high16<BF16>(u);
-    }
-  }
-}
-
 // The eight waves are two groups, one of each to a SIMD, that take turns: while one
 // has the matrix cores (the last tile's weights times V, then the next scores), the
 // other works its scores into weights, puts its share of a later tile into LDS and

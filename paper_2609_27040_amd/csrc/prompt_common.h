@@ -98,6 +98,25 @@ __device__ __forceinline__ float high16(uint32_t w) {
   else return float(__builtin_bit_cast(_Float16, uint16_t(w >> 16)));
 }
 
+// P of a tile in NP 16-bit parts whose sum keeps 8 (bf16) or 11 (f16) bits each.
+template <int NP>
+struct Weights {
+  u32x4 p[NP][4];        // [part][16 tokens]
+};
+
+template <bool BF16, int NP>
+__device__ __forceinline__ void put_weights(Weights<NP>& w, int ks, int q, float x, float y) {
+#pragma unroll
+  for (int n = 0; n < NP; ++n) {
+    const uint32_t u = pack16<BF16>(x, y);
+    w.p[n][ks][q] = u;
+    if (n + 1 < NP) {
+      x -= low16<BF16>(u);
+      y -= high16<BF16>(u);
+    }
+  }
+}
+
 // The value of the lane 32 away.
 __device__ __forceinline__ float other_half(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x),

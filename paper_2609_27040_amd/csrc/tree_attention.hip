@@ -30,25 +30,6 @@
 namespace ema {
 namespace {
 
-// P of a tile in NP 16-bit parts whose sum keeps 8 (bf16) or 11 (f16) bits each.
-template <int NP>
-struct Weights {
-  u32x4 p[NP][4];        // [part][16 tokens]
-};
-
-template <bool BF16, int NP>
-__device__ __forceinline__ void put_weights(Weights<NP>& w, int ks, int q, float x, float y) {
-#pragma unroll
-  for (int n = 0; n < NP; ++n) {
-    const uint32_t u = pack16<BF16>(x, y);
-    w.p[n][ks][q] = u;
-    if (n + 1 < NP) {
-      x -= low16<BF16>(u);
-      y -= high16<BF16>(u);
-    }
-  }
-}
-
 // Loads a tile of K or V into LDS, in the places of prompt_common.h. Its 16 pieces of 1 KiB are
 // shared out to RW waves; a lane's part of an address is the same for all of them but for the four
 // (K) or two (V) ways in which their 16-byte parts are turned, the rest is the wave's.
@@ -229,8 +210,6 @@ struct Segment {
 template <int ROWS>
 struct Shape;
 template <>
-struct Shape<32> { static constexpr int kWaves = 4, kPlaces = 1, kPerCu = 1; };
-template <>
 struct Shape<64> { static constexpr int kWaves = 4, kPlaces = 1, kPerCu = 2; };
 template <>
 struct Shape<128> { static constexpr int kWaves = 4, kPlaces = 2, kPerCu = 2; };
@@ -400,6 +379,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
 
   // ---- a segment's rows and tiles ----------------------------------------------------------
   int kvh = 0, first = 0, base = 0;          // of segment g; base: tokens before the nodes
+  bool alive = false;                        // the wave has rows
   int tok = -1, out_row = -1;                // the node of this lane's row, its row of out; -1: none
   const uint64_t inverse = (1ull << 32) / G + 1;         // x * inverse >> 32 = x / G for x < 2^16
   u32x4 q[8];
@@ -414,6 +394,9 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     const int r = first + rw * 32 + col, node0 = first / G, x = first - node0 * G + rw * 32 + col;
     const bool live = r < g.n * G;
     const int node = live ? node0 + int(x * inverse >> 32) : 0, h = live ? r - node * G : 0;
+    // (with 128 rows the branches cost more than the idle waves' products: 32 nodes of 4 heads behind
+    // 64 contexts 164 us for 155)
+    alive = ROWS == 128 || first + rw * 32 < g.n * G;
     tok = live ? node : -1;
     out_row = live ? (g.row0 + node) * a.q_heads + kvh * G + h : -1;
     const char* p = a.q + (int64_t(g.row0 + node) * a.q_stride + (kvh * G + h) * 128 + half * 8) * 2;
@@ -556,7 +539,6 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     st.open(a, g.b, kvh, j, g.len);
     at = st.blocks(j);
     load_k(j, 0);
-    if constexpr (RW == 1) load_v(j, 0);
     constexpr int kFirst = RW == 8 ? kPlaces - 1 : kPlaces;
 #pragma unroll
     for (int i = 1; i < kFirst; ++i) {
@@ -590,29 +572,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
     for (int ks = 0; ks < 8; ++ks) arrived(q[ks]);
     const bool counts = kvh == 0 && first == 0 && rw == 0;
     const int turns = (g.j1 - g.j0 + kGroups - 1) / kGroups;
-    if constexpr (RW == 1) {
-      for (int j = g.j0 + group; j < g.j1; j += kGroups) {
-        const bool more = j + kGroups < g.j1;
-        if (counts && st.window.bad != 0) st.count_bad(a, j, g.len);
-        loads_arrived_but_16();              // V of this tile is still on its way
-        scores(tile(0, 0));
-        if (is_partly(j)) hide(g, j, st.there(j, g.len));
-        reads_done();
-        const bool partly = is_partly(j);
-        const uint64_t there = partly ? st.there(j, g.len) : 0;
-        if (more) {
-          at = st.blocks(j + kGroups);
-          load_k(j + kGroups, 0);
-        }
-        softmax();
-        if (more) loads_arrived_but_16();    // the next tile's K is still on its way
-        else loads_arrived();
-        if (partly) odd |= st.template clean_v<BF16>(tile(0, 1), there, 0);
-        values(tile(0, 1));
-        reads_done();
-        if (more) load_v(j + kGroups, 0);
-      }
-    } else if constexpr (RW == 8) {
+    if constexpr (RW == 8) {
       // The eight waves are two groups, one of each to a SIMD, that take turns: while one has the
       // matrix cores (products), the other works its scores into weights and sends for later tiles,
       // V of the next but one and K of the one after it, into the places that the turns before were
@@ -643,15 +603,17 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
         __syncthreads();
       }
       for (int j = g.j0; j < g.j1; ++j) {
-        products(j > g.j0, tile(place(j - 1), 1), true, tile(place(j), 0));
+        if (alive) products(j > g.j0, tile(place(j - 1), 1), true, tile(place(j), 0));
         __syncthreads();
         send(j + late);
-        if (is_partly(j)) hide(g, j, st.there(j, g.len));
-        softmax();
+        if (alive) {
+          if (is_partly(j)) hide(g, j, st.there(j, g.len));
+          softmax();
+        }
         arrive(j + late);
         __syncthreads();
       }
-      products(true, tile(place(g.j1 - 1), 1), false, tile(0, 0));
+      if (alive) products(true, tile(place(g.j1 - 1), 1), false, tile(0, 0));
       if (!late) __syncthreads();
     } else {
       // K of a tile is sent for as soon as all are done with the scores of the one whose place it
@@ -672,8 +634,10 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
         }
         if (here) {
           if (counts && st.window.bad != 0) st.count_bad(a, j, g.len);
-          scores(tile(place, 0));
-          if (is_partly(j)) hide(g, j, st.there(j, g.len));
+          if (alive) {
+            scores(tile(place, 0));
+            if (is_partly(j)) hide(g, j, st.there(j, g.len));
+          }
         }
         reads_done();
         if (kPlaces > 1) {
@@ -686,14 +650,14 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
           at = st.blocks(last + kGroups);
           load_k(last + kGroups, place);
         }
-        if (here) softmax();
+        if (here && alive) softmax();
         if (kPlaces == 1) {
           if (more) loads_arrived_but<kNewer>();
           else loads_arrived();
           if (here) clean(g, j, place);
           __syncthreads();
         }
-        if (here) values(tile(place, 1));
+        if (here && alive) values(tile(place, 1));
         place = place == kPlaces - 1 ? 0 : place + 1;
       }
     }
@@ -871,7 +835,7 @@ __global__ __launch_bounds__(kJoinRows * 32) void tree_join(TreeAttnArgs a, int 
 Cut cut_of(const PromptArgs& a) {
   Cut c;
   const int64_t mean = (int64_t(a.tokens) + a.batch - 1) / a.batch * (a.q_heads / a.kv_heads);
-  c.rows = 32;
+  c.rows = 64;
   while (c.rows < 256 && c.rows < mean) c.rows *= 2;
   c.bound = tile_bound(a, c.rows) * a.kv_heads;
   // (the most that there can be tiles)
@@ -902,9 +866,6 @@ void launch_sizes(const TreeAttnArgs& a, const Cut& c, hipStream_t stream) {
 template <bool BF16, int NP>
 void launch_rows(const TreeAttnArgs& a, const Cut& c, hipStream_t stream) {
   switch (c.rows) {
-    case 32:
-      launch_sizes<BF16, NP, 32>(a, c, stream);
-      break;
     case 64:
       launch_sizes<BF16, NP, 64>(a, c, stream);
       break;
@@ -920,7 +881,7 @@ void launch_rows(const TreeAttnArgs& a, const Cut& c, hipStream_t stream) {
 
 bool tree_fits(const PromptArgs& a) {
   const int64_t tiles = (int64_t(a.max_blocks) * a.block_size + kKT - 1) / kKT;
-  return (tile_bound(a, 32) * a.kv_heads) * (tiles + kSegCost) < int64_t(1) << 30;
+  return (tile_bound(a, 64) * a.kv_heads) * (tiles + kSegCost) < int64_t(1) << 30;
 }
 
 size_t tree_workspace(const PromptArgs& a) {
