@@ -63,9 +63,13 @@ int ema_tree_tables(ema_slice_t h, const int32_t* parents, const int32_t* query_
  * [tokens][mask_words], 8-byte aligned, mask_words in [1, EMA_TREE_WORDS]. A row whose
  * own token is at a negative position gives zeros, and its request is counted.
  * The work is cut by the lengths: the same call gives the same bits, other lengths in
- * the batch may change the last ones. Any whole number of query heads per KV
- * head; tokens * num_q_heads below 2^29, batch up to 65535. Async on `stream`; `workspace` of
- * ema_paged_tree_workspace bytes for these sizes. Errors: INVAL, HIP.
+ * the batch may change the last ones, a wider table does not where both hold more
+ * than 512 tokens. The query heads of a KV head times a tree's nodes are best
+ * up to 256: further ones read the request's K and V again. Any whole number of query heads per KV
+ * head; tokens * num_q_heads below 2^29, batch up to 65535, and below 2^30: KV heads, times 64-token
+ * tiles of max_blocks and four, times 64-row tiles of all requests' nodes and heads of a
+ * group (INVAL otherwise). block_table may be NULL where max_blocks is 0. Async on `stream`;
+ * `workspace` of ema_paged_tree_workspace bytes for these sizes. Errors: INVAL, HIP.
  */
 int ema_paged_tree_workspace(ema_slice_t h, int32_t tokens, int32_t batch, int32_t num_q_heads,
                              int32_t max_blocks, size_t* bytes);

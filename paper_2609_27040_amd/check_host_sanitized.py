@@ -5,7 +5,7 @@ AddressSanitizer and UBSan (CPU only; no device code runs).
 
 Builds lib/host-sanitized/libema_slice.so, copies the packages and tests into
 a temporary directory with that library in place of the ordinary one, and
-runs the bookkeeping, slab, scheduling and ABI tests there with clang's ASan
+runs the bookkeeping, slab, scheduling, ABI and tree tests there with clang's ASan
 runtime preloaded; any report stops the run. Exits with pytest's status.
 """
 import glob
@@ -18,7 +18,7 @@ import tempfile
 from paper_2609_27040_amd.build import ROOT, build_host_sanitized
 
 TESTS = ["tests/test_host_logic.py", "tests/test_host_slab.py", "tests/test_sched.py",
-         "tests/test_abi.py"]
+         "tests/test_abi.py", "tests/test_tree_host.py"]
 
 
 def asan_runtime():

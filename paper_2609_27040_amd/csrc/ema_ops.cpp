@@ -226,7 +226,8 @@ int attention(const AttnCall& c) {
   if (c.tree && (c.mask_words < 1 || c.mask_words > EMA_TREE_WORDS))
     return inval(c.what, "mask_words must be in [1, EMA_TREE_WORDS]");
   if (c.tokens > 0 && c.batch > 0) {
-    if ((!h->host_only && (!c.q || !c.out)) || !c.block_table || !c.seq_lens ||
+    if ((!h->host_only && (!c.q || !c.out)) ||
+        (!c.block_table && (!c.tree || c.max_blocks > 0)) || !c.seq_lens ||
         (c.chunks && !c.query_start) || (c.maps == 2 && !h->host_only && !c.lambda))
       return inval(c.what, "NULL array");
     if (c.q_stride < int64_t(c.num_q_heads) * h->shape.head_dim || c.q_stride % 8 != 0)

@@ -1,8 +1,8 @@
 // Attention of drafted trees over the paged cache, on the matrix cores.
 //
 // The G query heads that share a KV head are rows beside each other: row r of a
-// request's n nodes is (node r / G, head r % G), and a workgroup takes 32 RT rows
-// past the request's tokens in tiles of 64, its four waves in turn:
+// request's n nodes is (node r / G, head r % G). 64, 128 or 256 rows (an item) go past the
+// request's tokens in tiles of 64 staged in LDS, 32 rows to a wave:
 //   scores   S^T[token][row] = K . Q^T     v_mfma_f32_32x32x16, A = 32 K rows, B = Q^T
 //            in registers; the rows of A are taken in an order that leaves every
 //            lane with 8 consecutive tokens of one row twice over
@@ -10,18 +10,34 @@
 //            and the lane 32 away the others
 //   output   O^T[channel][row] += V^T . P^T   A = 32 channels of the transposed V
 //            block, B = P as the scores left it: nothing moves between lanes
-// Each wave loads its own tiles, straight into its own 32 KiB of LDS, and keeps its own
-// maximum, sum and output; they are merged in the place of the tiles at the end.
+// Weights, their scale in f16 and the slack of the rescaling are those of the prompt
+// kernels (put_weights; below 2^8, with two f16 parts 2^4).
+//
+// What bounds it goes by the rows. 4 * 128 operations per (row, token): a KV head's token, 512
+// bytes, takes as long from HBM as some 200 rows' products. So an item has all rows of a tree,
+// up to 256 (a second tile of rows reads K and V again: 18 nodes of 4 heads behind 64 contexts take
+// 147 us as one item of 128 rows, 259 as two of 64), and as many workgroups run on a CU as their
+// tiles leave room for: two with 64 KiB of tiles each up to 128 rows, bound by HBM; one of two groups
+// of waves in turns with 256, bound by the matrix cores and HBM together. 64 trees of 16 nodes behind
+// 1024-4080 tokens (32 and 8 heads, bf16, 690 MB): 131 us, 5.3 TB/s. 32 trees of 64 nodes behind
+// 3000: 130 us, 770 TFLOP/s at 3.3 TB/s; its loads alone take 84 us, its products and softmax alone
+// 94, and what keeps them from overlapping better is not known (a place more, later waits: the same).
+//
+// Work: all items' tiles in a row, cut into equal shares, one a workgroup; items that several
+// share are joined by a second launch. Where whole items leave no workgroup with much more than
+// that, they stay whole: parts cost their rows' way to the workspace and back (64 trees of 16
+// nodes: 152 us shared, 136 whole). Work is cut by lengths and never by the table's width.
 //
 // Only tiles that reach past the older tokens look at the mask: 64 bits of it, those of
 // the tile's tokens, are shifted into place from two words of the row's. There V is
 // cleaned of what is not finite, since 0 times it would be NaN for rows that do not attend
-// it; where a tile has such values, a second product, of ones in their places and ones
-// for the attended tokens, tells which rows' channels become NaN.
+// it; where something was, the rows are looked at again at the end, value by value, and those
+// that do attend one get NaN in its channel.
 //
-// The output is rescaled only where a row's maximum has grown by more than 2^8; in f16
-// weights and their sum are kept in a power-of-two scale in which the largest stand just
-// below 2^15, as in the prompt kernels.
+// What did not help: 64 rows to a wave, one wave to a SIMD (half the LDS reads, but the registers
+// spill: 405 us for 254); 32-row items of four waves with a tile each (1 node 119 us for 124, but 8
+// nodes 131 for 126 and 4 nodes behind 200 contexts 163 for 145); ends of shares moved to the near
+// ends of items (152 for 150); eight waves or four workgroups on a CU for 64 rows (142, 150 for 135).
 #include "prompt_common.h"
 #include "tree_kernels.h"
 
@@ -154,10 +170,11 @@ struct TileLoader {
 };
 
 // Tiles that a segment costs a workgroup beyond its own: its queries, its first tiles' way from
-// HBM, its merge.
+// HBM, its merge. (8: within 2 % of 4 on eleven sizes.)
 constexpr int kSegCost = 4;
 constexpr int kCus = 256;
-constexpr int kWholeTiles = 8;           // tables of at most so many tiles: items are not shared
+constexpr int kWholeTiles = 8;           // tables of at most so many tiles: items are not shared, and
+                                         // there is no second launch
 constexpr int kRecord = 6;               // ints: see Record
 constexpr int kJoinRows = 8;
 constexpr int kJoinGrid = 4096;          // workgroups of the join that run at once
@@ -758,7 +775,8 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
 }
 
 // Joins the parts of shared items: 32 lanes to a row, four channels a lane; `share` such groups
-// of a workgroup take a row's parts in turn.
+// of a workgroup take a row's parts in turn. Bound by the parts' way from memory and by its chain of
+// loads: 41 MB of 16 trees of 48-64 nodes 15 us, 4.6 where nothing is shared.
 __global__ __launch_bounds__(kJoinRows * 32) void tree_join(TreeAttnArgs a, int grid, int rows,
                                                             int share) {
   __shared__ __attribute__((aligned(16))) f32x4 s_o[kJoinRows][32];
@@ -840,7 +858,11 @@ Cut cut_of(const PromptArgs& a) {
   c.bound = tile_bound(a, c.rows) * a.kv_heads;
   // (the most that there can be tiles)
   const int64_t tiles = (int64_t(a.max_blocks) * a.block_size + kKT - 1) / kKT;
+  // (7 nodes behind 32001 tokens, 8 and 1 heads: 30.5 us with shares of one tile, 23.9 with two and
+  // more, 25.7 with six; 31 nodes: 41.4 with one, 36.8 with two, 55 with sixteen)
   c.least = c.rows < 256 ? 6 : 4;
+  // (64 rows: HBM is full with half of the workgroups; 256: each has its own time. Several rounds of
+  // items are as uneven as one workgroup is alone with them: 200 requests, 8 heads, 204 us for 175)
   c.uneven = c.rows < 256 ? 8 : 5;
   const int64_t most_wgs = kCus * (c.rows == 64 ? Shape<64>::kPerCu : c.rows == 128 ? Shape<128>::kPerCu : 1);
   c.whole = tiles <= kWholeTiles && c.bound <= 1 << 16;

@@ -5,6 +5,9 @@
 // each, by doubling: after r rounds a lane has the bits of its 2^r nearest ancestors of
 // the block and the one above them. The block's highest ancestor hangs from a node of an
 // earlier block, whose own bits of that block are complete: at most one step a block.
+//
+// Both are chains of loads: 2.2 us for one request, 3.6 for 200 trees of 65-250 nodes (1.3 MB); the
+// rest of a call (7.7 us) is its launch and the binding.
 #include "tree_kernels.h"
 
 #include <algorithm>

@@ -759,6 +759,8 @@ def paged_tree_attention(h, q, query_start, block_table, seq_lens, mask, out, sc
     """Attention of drafted nodes: mask int64 [T][words] says which of its request's nodes a
     row attends beside all tokens before them (bit j: the node in the j-th of the request's
     rows, which are its last tokens); the other arrays as in paged_prompt_attention."""
+    if mask is None:
+        _bad("mask: missing")
     _attention_op(h, _lib.ema_paged_tree_attention, _lib.ema_paged_tree_workspace, 1, q,
                   query_start, block_table, seq_lens, out, scale, None, None, 0.0, full_weights,
                   workspace, stream, mask)

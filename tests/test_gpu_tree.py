@@ -209,6 +209,41 @@ def test_attention_matches_the_oracle(ema, case, out, full_weights):
         k.close()
 
 
+@pytest.mark.parametrize("heads,new", [((300, 1), [2, 1]), ((1030, 2), [1, 2]), ((64, 1), [40, 9])])
+def test_large_groups(ema, heads, new):
+    """Row tiles that begin and end inside a node's heads."""
+    k = Case(ema, [70, 600], new, heads, 16, "bf16", seed=14)
+    try:
+        k.check(k.call(k.out(torch.float32)))
+        k.check(k.call(k.out(torch.bfloat16)))
+    finally:
+        k.close()
+
+
+@pytest.mark.parametrize("lens,new", [([40] * 700, [3] * 700), ([20000], [70]), ([9000, 3, 70, 1], [5, 3, 64, 1]),
+                                      ([1500] * 70 + [1], [2] * 70 + [1])])
+def test_many_requests_and_long_ones(ema, lens, new):
+    """Whole items, equal shares of them, and a few in many parts; requests without nodes too."""
+    k = Case(ema, lens, new, (4, 2), 16, "bf16", seed=15)
+    try:
+        k.check(k.call(k.out(torch.float32)))
+        assert ema.slice_device_errors(k.c.h) == 0
+    finally:
+        k.close()
+
+
+def test_an_empty_table_gives_zeros(ema):
+    c = SmallCache(ema, [5], 2, 16, "bf16")
+    try:
+        o = torch.full((3, 4, D), 7.0, device="cuda")
+        ema.paged_tree_attention(c.h, dev16(c.queries(3, 4), "bf16"), i32([0, 3]),
+                                 torch.empty((1, 0), dtype=torch.int32, device="cuda"), i32([0]),
+                                 full((3, 1), -1, torch.int64), o)
+        assert (o == 0).all() and ema.slice_device_errors(c.h) == 1    # more nodes than tokens
+    finally:
+        c.close()
+
+
 def test_a_16_bit_output_of_the_other_type(ema):
     k = Case(ema, [333, 20], [9, 20], (4, 2), 16, "f16", seed=3)
     try:
@@ -498,6 +533,40 @@ def test_compaction_matches_the_oracle(ema, case, layout):
         assert ema.slice_device_errors(p.h) == 0
     finally:
         p.close()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+def test_empty_lists_and_tables(ema, layout):
+    p = Pools(ema, 1, [20, 20], 1, 16, layout, 0.5)
+    try:
+        new = full((2,))
+        none = torch.empty((2, 0), dtype=torch.int32, device="cuda")
+        ema.kv_compact(p.h, i32(p.table), i32([3, 0]), none, i32([0, 0]), new_lens=new)
+        assert new.cpu().tolist() == [3, 0]
+        ema.kv_compact(p.h, none[None], i32([0, 0]), i32([[0, 1], [5, 6]]), i32([0, 2]), new_lens=new)
+        assert new.cpu().tolist() == [0, 2] and ema.slice_device_errors(p.h) == 2
+        p.same()
+    finally:
+        p.close()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+def test_many_lists_long_and_short(ema, layout):
+    """More requests than are put in order of their lists, and as many."""
+    for B in (256, 300):
+        rng = np.random.default_rng(B)
+        lens = rng.integers(12, 130, B)
+        p = Pools(ema, 1, lens, 1, 16, layout, 0.4, seed=B)
+        try:
+            base = rng.integers(0, 12, B)
+            counts = [int(rng.integers(0, n - b + 1)) for n, b in zip(lens, base)]
+            keep = lists(p.rng, base, lens, counts)
+            ema.kv_compact(p.h, i32(p.table), i32(base), i32(keep), i32(counts))
+            p.expect(base, keep, counts)
+            p.same()
+            assert ema.slice_device_errors(p.h) == 0
+        finally:
+            p.close()
 
 
 @pytest.mark.parametrize("layout", [0, 1])
