@@ -9,8 +9,9 @@
 // 32 to 128 bytes with its neighbours, and memory moves them whole.
 //
 // No arithmetic: bound by memory's lines and, long lists, by the chain list - table - tokens of a
-// chunk. Accepted paths of 64 requests (4 of 16 nodes, 32 layers, 8 heads, 50 MB of K and V): 50-56
-// us, 43 of them the kernel, which moves 57 MB in and 111 out (FETCH_SIZE, WRITE_SIZE: V's lines).
+// chunk. Accepted paths of 64 requests (4 of 16 nodes, 32 layers, 8 heads, 50 MB of K and V): 50-57
+// us, 43 of them the kernel, which writes 113 MB for V's lines (WRITE_SIZE) and reads some 117
+// (FETCH_SIZE twice: it counts half of wide reads; not calibrated for narrow ones).
 // 8 contexts of 901-3501 tokens thinned to half (80 layers, 718 MB): 205 us, 3.5 TB/s.
 #include "tree_kernels.h"
 

@@ -26,7 +26,8 @@
 // Work: all items' tiles in a row, cut into equal shares, one a workgroup; items that several
 // share are joined by a second launch. Where whole items leave no workgroup with much more than
 // that, they stay whole: parts cost their rows' way to the workspace and back (64 trees of 16
-// nodes: 152 us shared, 136 whole). Work is cut by lengths and never by the table's width.
+// nodes: 152 us shared, 136 whole). Work is cut by lengths, not by the
+// table's width, but for tables of at most 512 tokens, whose items all stay whole.
 //
 // Only tiles that reach past the older tokens look at the mask: 64 bits of it, those of
 // the tile's tokens, are shifted into place from two words of the row's. There V is
@@ -776,7 +777,7 @@ __global__ __launch_bounds__(Shape<ROWS>::kWaves * 64, 2) void tree_kernel(TreeA
 
 // Joins the parts of shared items: 32 lanes to a row, four channels a lane; `share` such groups
 // of a workgroup take a row's parts in turn. Bound by the parts' way from memory and by its chain of
-// loads: 41 MB of 16 trees of 48-64 nodes 15 us, 4.6 where nothing is shared.
+// loads: 41 MB of 16 trees of 48-64 nodes 16 us, 4.6 where nothing is shared.
 __global__ __launch_bounds__(kJoinRows * 32) void tree_join(TreeAttnArgs a, int grid, int rows,
                                                             int share) {
   __shared__ __attribute__((aligned(16))) f32x4 s_o[kJoinRows][32];
