@@ -112,6 +112,7 @@ class Tree(Chunk):
             if (p < -1).any() or (p >= np.arange(len(p))).any():
                 raise ValueError("parents: each below its node, -1 for a root")
         super().__init__(cache, [len(p) for p in trees], stream)
+        self.old = cache.lens - self.new
         words = max(1, -(-max(map(len, trees), default=0) // 64))
         self.parents = _dev(np.concatenate(trees + [np.zeros(0, np.int64)]))
         i32 = dict(dtype=torch.int32, device="cuda")
@@ -327,15 +328,23 @@ class PagedKVCache:
     def commit(self, tree, path, n_path, stream=None):
         """Keeps the nodes of each sequence's path (ascending) of its tree: their K and V follow
         the tokens before it in every layer, and the lengths are those tokens and the path.
-        Works on the canonical tables, so the layers' writebacks come before it. Waits for
-        the lengths, which the host keeps too."""
+        Works on the canonical tables as ``self.tables`` has them now, so the layers'
+        writebacks come before it. Waits for the lengths, which the host keeps too."""
         tree.used_on(stream)
         there = ema.torch_stream(stream)
+        # of each sequence the blocks that its nodes are in, in one upload
+        B, first, end = self.B, tree.old // self.bs, -(-(tree.old + tree.new) // self.bs)
+        j = first[:, None] + np.arange((end - first).max(initial=1))
+        ids = self.tables[:, np.arange(B)[:, None], np.minimum(j, self.tables.shape[2] - 1)]
+        before = first * self.bs
         with torch.cuda.stream(there):
-            lens = torch.empty(self.B, dtype=torch.int32, device="cuda")
-            ema.kv_compact(self.h, self.tables_dev, tree.base, path, n_path, new_lens=lens,
+            sent = _dev(np.concatenate([np.where(j < end[:, None], ids, -1).ravel(),
+                                        tree.old - before, before]))
+            table, base, before = sent.split([ids.size, B, B])
+            lens = torch.empty(B, dtype=torch.int32, device="cuda")
+            ema.kv_compact(self.h, table.view(ids.shape), base, path, n_path, new_lens=lens,
                            stream=stream)
-            self.lens_dev.copy_(lens)
+            self.lens_dev.copy_(lens.add_(before))
             self.lens = lens.cpu().numpy().astype(np.int64)
 
     def new_token_kv(self, seed=0):
