@@ -18,7 +18,7 @@ import tempfile
 from paper_2609_27040_amd.build import ROOT, build_host_sanitized
 
 TESTS = ["tests/test_host_logic.py", "tests/test_host_slab.py", "tests/test_sched.py",
-         "tests/test_abi.py", "tests/test_tree_host.py"]
+         "tests/test_abi.py", "tests/test_tree_host.py", "tests/test_tree_host_bounds.py"]
 
 
 def asan_runtime():

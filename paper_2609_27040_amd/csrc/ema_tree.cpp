@@ -32,9 +32,11 @@ int check_trees(const ema_slice* h, const char* what, const int32_t* parents,
   if (starts[0] != 0 || starts[batch] > tokens)
     return inval(what, "query_start must run from 0 to at most the number of tokens");
   for (int32_t b = 0; b < batch; ++b) {
+    // (compared before they are subtracted; an entry past the last one would be read if the
+    // starts did not ascend)
+    if (starts[b + 1] < starts[b] || starts[b + 1] > tokens)
+      return inval(what, "query_start descends");
     const int32_t n = starts[b + 1] - starts[b];
-    // (an entry past the last one would be read if the starts did not ascend)
-    if (n < 0 || starts[b + 1] > tokens) return inval(what, "query_start descends");
     if (seq_lens && lens[b] < n) return inval(what, "more nodes than the request has tokens");
     if (n > most) return inval(what, "more nodes than are looked at");
     for (int32_t i = 0; i < n; ++i)
