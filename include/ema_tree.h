@@ -114,7 +114,7 @@ int ema_tree_accept(ema_slice_t h, const int32_t* parents, const int32_t* query_
  * block_table: device int32 [layers][batch][max_blocks] unified ids of the canonical
  * tables: blocks are changed where they live, in either pool and the slice's
  * layout; staged copies stay as they were. No block may be named twice among those that
- * tokens from base[b] on are in. base, n_keep [batch], keep [batch][keep_cap],
+ * moved tokens come from or go to. base, n_keep [batch], keep [batch][keep_cap],
  * new_lens: device int32; new_lens must not overlap the inputs. A negative base,
  * n_keep outside [0, keep_cap] (clamped), an entry that does not ascend or lies past the table, and a
  * table entry outside both pools that a moved token is in, are counted (the

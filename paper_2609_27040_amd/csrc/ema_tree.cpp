@@ -4,6 +4,10 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <utility>
+#include <vector>
+
 #include "op_checks.h"
 #include "slice_handle.h"
 #include "tree_kernels.h"
@@ -58,7 +62,9 @@ int check_lists(const ema_slice* h, const int32_t* block_table, const int32_t* b
       (rc = count.get(h, n_keep, batch, st)))
     return rc;
   const int32_t bs = h->shape.block_size, all = h->book.n_local() + h->book.n_slice();
+  std::vector<std::pair<int32_t, int64_t>> used;   // a block, the entry that names it
   for (int32_t b = 0; b < batch; ++b) {
+    const auto mine = int64_t(used.size());
     if (first[b] < 0) return inval(what, "a negative base");
     if (count[b] < 0 || count[b] > keep_cap) return inval(what, "n_keep outside [0, keep_cap]");
     for (int32_t k = 0; k < count[b]; ++k) {
@@ -70,11 +76,18 @@ int check_lists(const ema_slice* h, const int32_t* block_table, const int32_t* b
       if (list[e] == k) continue;
       for (int32_t l = 0; l < layers; ++l)
         for (int64_t t : {from, int64_t(first[b]) + k}) {
-          const int32_t id = table[(int64_t(l) * batch + b) * max_blocks + t / bs];
-          if (id < 0 || id >= all) return inval(what, "a table entry outside both pools");
+          const int64_t at = (int64_t(l) * batch + b) * max_blocks + t / bs;
+          if (table[at] < 0 || table[at] >= all)
+            return inval(what, "a table entry outside both pools");
+          used.emplace_back(table[at], at);
         }
     }
+    std::sort(used.begin() + mine, used.end());    // (a block has many tokens)
+    used.erase(std::unique(used.begin() + mine, used.end()), used.end());
   }
+  std::sort(used.begin(), used.end());
+  for (size_t i = 1; i < used.size(); ++i)
+    if (used[i].first == used[i - 1].first) return inval(what, "a block named twice");
   return EMA_OK;
 }
 

@@ -1,5 +1,5 @@
 """Refusals of the operators of include/ema_tree.h on the host: starts at the ends of their
-type."""
+type, blocks named twice."""
 import numpy as np
 import pytest
 
@@ -16,3 +16,22 @@ def test_starts_at_the_ends_of_their_type(host, starts):
             refused(ema, ema.tree_tables, h, z(2) - 1, i32(starts), i32([HIGH, HIGH]), _Mask(2, 1)),
             refused(ema, ema.tree_accept, h, z(2) - 1, i32(starts), z(2), z(2), z(2, 3), z(2), z(2))):
         assert "query_start" in message
+
+
+def test_a_block_named_twice_is_refused(host):
+    ema, h = host
+
+    def f(table, base, keep, n):
+        ema.kv_compact(h, i32(table), i32(base), i32(keep), i32(n))
+
+    two = [[0, 17, 18, -1], [1, 20, 47, -1]]
+    f([[[0, 1, -1], [13, 3, 17]]], [0, 0], two, [3, 3])
+    f([[[0, 1, 5], [13, 3, 5]]], [0, 0], two, [3, 0])                  # no token of the second request
+    f([[[0, 1, 5], [0, 1, 5]]], [0, 0], [[0, 1, 2], [1, 2, 4]], [3, 3])    # nor of the first
+    f([[[0, 1, 4], [13, 3, 4]]], [0, 0], [[0, 17, 18], [1, 2, 31]], [3, 3])  # not moved there
+    bad = [([[[0, 0, -1], [13, 3, 17]]], [3, 3]),                      # of one request
+           ([[[0, 1, -1], [13, 3, 1]]], [3, 3]),                       # of two
+           ([[[0, 1, -1], [13, 3, 17]], [[2, 4, -1], [14, 0, 16]]], [3, 3])]     # of two layers
+    for table, n in bad:
+        assert "twice" in refused(ema, f, table, [0, 0], two, n)
+    f([[[0, 1, -1], [13, 3, 17]], [[2, 4, -1], [14, 5, 16]]], [0, 0], two, [3, 3])
