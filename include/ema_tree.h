@@ -38,7 +38,7 @@ extern "C" {
  * parents, query_start [batch + 1], seq_lens [batch]: device int32; mask: device
  * uint64 [tokens][mask_words], 8-byte aligned; positions [tokens], base [batch]: device
  * int32. Rows behind the last start stay as they were. Outputs must not overlap
- * each other or the inputs. A parent that is not below its node, or below -1, makes a root,
+ * each other or the inputs (INVAL). A parent that is not below its node, or below -1, makes a root,
  * counted; nodes from 64 * mask_words on get no bits and base as their position, their
  * request is counted; so is one with a length below n_b (base is negative then) and,
  * clamped, one whose starts are no range of the rows. mask_words in [1,
@@ -93,7 +93,7 @@ int ema_paged_tree_attention(ema_slice_t h, const void* q, int64_t q_stride,
  *                without root_choice (a request without nodes)
  * All arrays are device int32: parents, drafted, choice [tokens], query_start [batch +
  * 1], root_choice [batch], path [batch][path_cap], n_path, next [batch]. Outputs must not
- * overlap each other or the inputs. Parents as for ema_tree_tables, those out of range make
+ * overlap each other or the inputs (INVAL). Parents as for ema_tree_tables, those out of range make
  * nodes that no path reaches, counted; nodes from EMA_TREE_NODES on are not looked
  * at and their request is counted. path_cap at least 1, batch up to 65535. Async on
  * `stream`. Errors: INVAL (in checked mode and host-only also bad parents or starts), HIP.
@@ -115,7 +115,7 @@ int ema_tree_accept(ema_slice_t h, const int32_t* parents, const int32_t* query_
  * tables: blocks are changed where they live, in either pool and the slice's
  * layout; staged copies stay as they were. No block may be named twice among those that
  * moved tokens come from or go to. base, n_keep [batch], keep [batch][keep_cap],
- * new_lens: device int32; new_lens must not overlap the inputs. A negative base,
+ * new_lens: device int32; new_lens must not overlap the inputs (INVAL). A negative base,
  * n_keep outside [0, keep_cap] (clamped), an entry that does not ascend or lies past the table, and a
  * table entry outside both pools that a moved token is in, are counted (the
  * entries once for every layer and moved token there) and those tokens not moved. layers in [1, 65535], batch up to 65535,

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <utility>
 #include <vector>
 
@@ -22,6 +23,26 @@ using ema::must_check;
 namespace {
 
 constexpr int32_t kMostBatch = 65535;
+
+// n elements of an array, which may be missing.
+struct Span {
+  uintptr_t from, to;
+  template <typename T>
+  Span(const T* p, int64_t n)
+      : from(reinterpret_cast<uintptr_t>(p)), to(p && n > 0 ? from + uintptr_t(n) * sizeof(T) : from) {}
+  bool meets(const Span& o) const { return from < o.to && o.from < to; }
+};
+
+// Outputs that overlap each other or an input: a workgroup would read what another has written.
+bool overlap(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
+  for (const Span* a = outputs.begin(); a != outputs.end(); ++a) {
+    for (const Span* b = a + 1; b != outputs.end(); ++b)
+      if (a->meets(*b)) return true;
+    for (const Span& b : inputs)
+      if (a->meets(b)) return true;
+  }
+  return false;
+}
 
 // The starts and, of the nodes that are looked at, the parents.
 int check_trees(const ema_slice* h, const char* what, const int32_t* parents,
@@ -107,6 +128,9 @@ int ema_tree_tables(ema_slice_t h, const int32_t* parents, const int32_t* query_
   if (!query_start || !seq_lens || (tokens > 0 && !parents)) return inval(what, "NULL array");
   if (!h->host_only && tokens > 0 && (!mask || reinterpret_cast<uintptr_t>(mask) % 8 != 0))
     return inval(what, "mask missing or not 8-byte aligned");
+  if (overlap({{mask, int64_t(tokens) * mask_words}, {positions, tokens}, {base, batch}},
+              {{parents, tokens}, {query_start, int64_t(batch) + 1}, {seq_lens, batch}}))
+    return inval(what, "an output overlaps another or an input");
   hipStream_t st = static_cast<hipStream_t>(stream);
   DeviceScope ds;
   if (!h->host_only)
@@ -147,6 +171,10 @@ int ema_tree_accept(ema_slice_t h, const int32_t* parents, const int32_t* query_
   if (!query_start || (tokens > 0 && !parents)) return inval(what, "NULL array");
   if (!h->host_only && ((tokens > 0 && (!drafted || !choice)) || !path || !n_path || !next))
     return inval(what, "NULL array");
+  if (overlap({{path, int64_t(batch) * path_cap}, {n_path, batch}, {next, batch}},
+              {{parents, tokens}, {query_start, int64_t(batch) + 1}, {drafted, tokens},
+               {choice, tokens}, {root_choice, batch}}))
+    return inval(what, "an output overlaps another or an input");
   hipStream_t st = static_cast<hipStream_t>(stream);
   DeviceScope ds;
   if (!h->host_only)
@@ -190,6 +218,10 @@ int ema_kv_compact(ema_slice_t h, const int32_t* block_table, const int32_t* bas
     return inval(what, "batch * max_blocks * block_size must be below 2^31");
   if (!base || !n_keep || (keep_cap > 0 && !keep) || (max_blocks > 0 && !block_table))
     return inval(what, "NULL array");
+  if (overlap({{new_lens, batch}},
+              {{block_table, int64_t(layers) * batch * max_blocks}, {base, batch},
+               {keep, int64_t(batch) * keep_cap}, {n_keep, batch}}))
+    return inval(what, "new_lens overlaps an input");
   hipStream_t st = static_cast<hipStream_t>(stream);
   DeviceScope ds;
   if (!h->host_only)

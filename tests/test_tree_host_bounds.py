@@ -1,5 +1,5 @@
 """Refusals of the operators of include/ema_tree.h on the host: starts at the ends of their
-type, blocks named twice."""
+type, blocks named twice, outputs that overlap other arrays."""
 import numpy as np
 import pytest
 
@@ -35,3 +35,35 @@ def test_a_block_named_twice_is_refused(host):
     for table, n in bad:
         assert "twice" in refused(ema, f, table, [0, 0], two, n)
     f([[[0, 1, -1], [13, 3, 17]], [[2, 4, -1], [14, 5, 16]]], [0, 0], two, [3, 3])
+
+
+def test_outputs_that_overlap_are_refused(host):
+    ema, h = host
+    starts, lens = i32([0, 2, 5]), i32([9, 9])
+
+    def tables(parents=z(5) - 1, seq_lens=lens, **out):
+        ema.tree_tables(h, parents, starts, seq_lens, _Mask(5, 1), **out)
+
+    p, both = z(5) - 1, z(7)
+    tables(p, positions=z(5), base=z(2))
+    tables(p, positions=both[:5], base=both[5:])                       # side by side
+    for out in (dict(base=lens), dict(base=starts[1:]), dict(positions=p), dict(base=p[3:]),
+                dict(positions=both[:5], base=both[4:6])):
+        assert "overlaps" in refused(ema, tables, p, **out)
+
+    def accept(path=None, n_path=None, next_token=None, root=None):
+        ema.tree_accept(h, p, starts, p, p, z(2, 3) if path is None else path,
+                        z(2) if n_path is None else n_path, z(2) if next_token is None else next_token,
+                        root_choice=root)
+
+    wide, two = z(10), z(2)
+    accept(wide[:6].reshape(2, 3), wide[6:8], wide[8:])
+    for a in (dict(path=wide[:6].reshape(2, 3), n_path=wide[5:7]), dict(n_path=two, next_token=two),
+              dict(next_token=two, root=two), dict(n_path=p[:2]), dict(next_token=starts[:2])):
+        assert "overlaps" in refused(ema, accept, **a)
+
+    table, keep = i32([[[0, 1], [2, 3]]]), i32([[1, 5], [0, 3]])
+    base, n = i32([0, 3]), i32([2, 2])
+    ema.kv_compact(h, table, base, keep, n, new_lens=z(2))
+    for out in (base, n, keep[1], table[0, 0]):
+        assert "overlaps" in refused(ema, ema.kv_compact, h, table, base, keep, n, new_lens=out)
