@@ -599,7 +599,7 @@ def _attention_op(h, fn, size, maps, q, query_start, block_table, seq_lens, out,
     if rec[0] if rec else _host_only(h):
         table, lens = _i32_host(block_table), _i32_host(seq_lens)
         starts = () if query_start is None else (_i32_host(query_start).ctypes.data,)
-        masks = () if mask is None else (None, mask.shape[1])
+        masks = () if mask is None else (None, _mask_shape(mask, rows))
         _check(fn(h, None, Hq * 128, *starts, table.ctypes.data, lens.ctypes.data, *masks, *sizes,
                   float(scale), *extra, None, F32, None, 0, None))
         return
@@ -720,12 +720,18 @@ def _rows_and_batch(parents, query_start):
     return rows, B - 1
 
 
-def _mask_words(mask, rows):
-    """(address, words) of the masks of `rows` rows."""
+def _mask_shape(mask, rows):
+    """Words of the masks of `rows` rows."""
     shape = mask.shape
     if len(shape) != 2 or shape[0] != rows:
         _bad(f"mask: shape {tuple(shape)}, expected [{rows}][words]")
-    return _dev(mask, "mask", _torch().i64), shape[1]
+    return shape[1]
+
+
+def _mask_words(mask, rows):
+    """(address, words) of the masks of `rows` rows."""
+    words = _mask_shape(mask, rows)
+    return _dev(mask, "mask", _torch().i64), words
 
 
 def tree_tables(h, parents, query_start, seq_lens, mask, positions=None, base=None, stream=None):
@@ -741,10 +747,7 @@ def tree_tables(h, parents, query_start, seq_lens, mask, positions=None, base=No
                             ("seq_lens", seq_lens, B), ("positions", positions, rows),
                             ("base", base, B)))
     if host:
-        shape = mask.shape
-        if len(shape) != 2 or shape[0] != rows:
-            _bad(f"mask: shape {tuple(shape)}, expected [{rows}][words]")
-        at, words, st = None, shape[1], None
+        at, words, st = None, _mask_shape(mask, rows), None
     else:
         (at, words), st = _mask_words(mask, rows), _stream(stream)
     _check(_lib.ema_tree_tables(h, *addr[:3], rows, B, at, words, *addr[3:], st))

@@ -1,9 +1,10 @@
 """Refusals of the operators of include/ema_tree.h on the host: starts at the ends of their
-type, blocks named twice, outputs that overlap other arrays."""
+type, blocks named twice, outputs that overlap other arrays,
+masks of another shape."""
 import numpy as np
 import pytest
 
-from test_tree_host import _Mask, host, i32, pytestmark, refused, z  # noqa: F401
+from test_tree_host import _Mask, _Q, host, i32, pytestmark, refused, z  # noqa: F401
 
 LOW, HIGH = -2 ** 31, 2 ** 31 - 1
 
@@ -67,3 +68,12 @@ def test_outputs_that_overlap_are_refused(host):
     ema.kv_compact(h, table, base, keep, n, new_lens=z(2))
     for out in (base, n, keep[1], table[0, 0]):
         assert "overlaps" in refused(ema, ema.kv_compact, h, table, base, keep, n, new_lens=out)
+
+
+def test_masks_of_another_shape(host):
+    ema, h = host
+    f = lambda mask: ema.paged_tree_attention(h, _Q(8, 4), i32([0, 8]), i32([[0, 1]]), i32([20]), mask,
+                                              None)
+    f(_Mask(8, 1))
+    for shape in ((), (8,), (7, 1), (9, 1), (8, 1, 1)):
+        assert "mask" in refused(ema, f, _Mask(*shape))
