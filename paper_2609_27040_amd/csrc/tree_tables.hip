@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kThreads) void tree_tables_kernel(TreeTablesArgs a)
   const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x;
   int s, n;
   const int wrong = rows_of(a.starts, a.tokens, b, s, n);
-  const int given = a.seq_lens[b], base = given - n;
+  const int given = a.seq_lens[b], base = max(given, INT_MIN + n) - n;
   const int known = min(n, 64 * a.words);
   if (tid == 0) {
     if (a.base) a.base[b] = base;
