@@ -118,9 +118,11 @@ int ema_tree_accept(ema_slice_t h, const int32_t* parents, const int32_t* query_
  * new_lens: device int32; new_lens must not overlap the inputs (INVAL). A negative base,
  * n_keep outside [0, keep_cap] (clamped), an entry that does not ascend or lies past the table, and a
  * table entry outside both pools that a moved token is in, are counted (the
- * entries once for every layer and moved token there) and those tokens not moved. layers in [1, 65535], batch up to 65535,
- * batch * max_blocks * block_size below 2^31. Async on `stream`. Errors: INVAL (in checked mode and
- * host-only also any of the violations above), HIP.
+ * entries once for every layer and moved token there) and those tokens not moved. Arrays of up to
+ * nine columns (keep_cap) take a form for short lists that is several times faster.
+ * layers in [1, 65535], batch up to 65535, batch * max_blocks * block_size below 2^31. Async
+ * on `stream`. Errors: INVAL (in checked mode and host-only also any of the violations
+ * above), HIP.
  */
 int ema_kv_compact(ema_slice_t h, const int32_t* block_table, const int32_t* base,
                    const int32_t* keep, const int32_t* n_keep, int32_t layers, int32_t batch,

@@ -10,8 +10,10 @@
 //
 // No arithmetic: bound by memory's lines and, long lists, by the chain list - table - tokens of a
 // chunk. Accepted paths of 64 requests (4 of 16 nodes, 32 layers, 8 heads, 50 MB of K and V): 50-57
-// us, 43 of them the kernel, which writes 113 MB for V's lines (WRITE_SIZE) and reads some 117
-// (FETCH_SIZE twice: it counts half of wide reads; not calibrated for narrow ones).
+// us, nearly all of them the kernel, which writes 112 MB for V's lines (WRITE_SIZE) and reads 58 to
+// 115 (FETCH_SIZE, or twice: it counts half of wide reads, and is not calibrated for narrow ones).
+// 43 us where the call before has left the lines in the last-level cache. The same paths in an array
+// of ten columns or more are a long list's work: 390 us.
 // 8 contexts of 901-3501 tokens thinned to half (80 layers, 718 MB): 205 us, 3.5 TB/s.
 #include "tree_kernels.h"
 
@@ -24,7 +26,11 @@ namespace {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;            // that move
-constexpr int kShort = 9;                // entries of a short list
+// Columns of `keep` up to which the lists are short ones, whatever is in them. That there is such a
+// border: 64 requests, 32 layers, 8 heads, all lists of 4 entries 50 us as short ones, 388 as long
+// ones; of 9, 92 and 409. It is not the best one: short lists' form takes 126 us for 12 entries, 160
+// for 16 and 272 for 28 (with room for 32), the long ones' 415, 422 and 442.
+constexpr int kShort = 9;
 constexpr int kBuffers = 4;
 
 // Where a token is read or written.

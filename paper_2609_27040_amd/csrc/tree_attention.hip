@@ -19,9 +19,14 @@
 // 147 us as one item of 128 rows, 259 as two of 64), and as many workgroups run on a CU as their
 // tiles leave room for: two with 64 KiB of tiles each up to 128 rows, bound by HBM; one of two groups
 // of waves in turns with 256, bound by the matrix cores and HBM together. 64 trees of 16 nodes behind
-// 1024-4080 tokens (32 and 8 heads, bf16, 690 MB): 131 us, 5.3 TB/s. 32 trees of 64 nodes behind
-// 3000: 130 us, 770 TFLOP/s at 3.3 TB/s; its loads alone take 84 us, its products and softmax alone
-// 94, and what keeps them from overlapping better is not known (a place more, later waits: the same).
+// 1024-4080 tokens (32 and 8 heads, bf16, 690 MB): 131 us, 5.3 TB/s; its loads alone take 128, its
+// products and softmax alone 70. 32 trees of 64 nodes behind 3000: 136 us, 740 TFLOP/s at 3.2 TB/s;
+// loads alone 83, products and softmax alone 100, and what keeps them from overlapping better is
+// not known (a place more, later waits: the same).
+//
+// Weights of 32-bit accuracy do not fit beside outputs and scores: in three parts (bf16) every form
+// spills, 12 to 120 bytes a lane, in two (f16) four of nine, up to 52; in one part none does. The
+// 64 trees of 16 nodes with 32-bit outputs: 170 us (f16 158), of 64 nodes 356 for 255.
 //
 // Work: all items' tiles in a row, cut into equal shares, one a workgroup; items that several
 // share are joined by a second launch. Where whole items leave no workgroup with much more than
@@ -859,8 +864,11 @@ Cut cut_of(const PromptArgs& a) {
   c.bound = tile_bound(a, c.rows) * a.kv_heads;
   // (the most that there can be tiles)
   const int64_t tiles = (int64_t(a.max_blocks) * a.block_size + kKT - 1) / kKT;
-  // (7 nodes behind 32001 tokens, 8 and 1 heads: 30.5 us with shares of one tile, 23.9 with two and
-  // more, 25.7 with six; 31 nodes: 41.4 with one, 36.8 with two, 55 with sixteen)
+  // (one request of 8 and 1 heads. 7 nodes behind 32001 tokens: 29.5 us with 2 units, 24.4 with 4,
+  // 23.3 with 6, 23.9 with 8, 29.2 with 16; behind 8001: 19.5, 18.4, 19.7, 21.4, 28.0. 15 nodes: 38.6,
+  // 31.8, 32.1, 33.8, 44.9 and 23.3, 24.5, 26.9, 30.1, 43.5. 31 nodes, 256 rows, behind 32001: 41.1,
+  // 37.1, 37.2, 39.8, 49.6. So 6 is at most 3 % off the best behind long contexts, and some 2 us
+  // behind shorter ones, where 4 or fewer would do)
   c.least = c.rows < 256 ? 6 : 4;
   // (64 rows: HBM is full with half of the workgroups; 256: each has its own time. Several rounds of
   // items are as uneven as one workgroup is alone with them: 200 requests, 8 heads, 204 us for 175)
