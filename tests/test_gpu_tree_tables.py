@@ -176,3 +176,22 @@ def test_paths_as_long_as_the_trees(layout):
         assert max(k.max() for k in kept) > 2
     finally:
         w.close()
+
+
+@pytest.mark.parametrize("checked", [False, True])
+def test_steps_without_nodes_and_full_tables(checked):
+    """No sequence has nodes; one has filled its table; one is empty; then all of a table is nodes."""
+    s = Server(0, False, checked=checked)
+    w = s.w
+    try:
+        full = w.tables.shape[2] * w.bs
+        s.base = np.array([full, 0, 90, 170])
+        assert s.step([0, 0, 0, 0], cap=None).tolist() == [0, 0, 0, 0]
+        assert s.base.tolist() == [full, 0, 90, 170]
+        s.base[0] = full - 33
+        s.step([33, 1, 0, 5], cap=None)
+        s.free(0, 0)
+        s.base[0] = 0
+        s.step([full, 0, 2, 1])
+    finally:
+        w.close()
